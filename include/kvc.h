@@ -47,7 +47,8 @@ typedef enum {
   KVC_ERR_UNSUPPORTED = -2, /* shape outside what the kernels handle (see kvc_desc) */
   KVC_ERR_WORKSPACE = -3,   /* workspace missing, misaligned or smaller than kvc_workspace_size */
   KVC_ERR_CUDA = -4,        /* a CUDA runtime call failed; message in kvc_last_error() */
-  KVC_ERR_TIMEOUT = -5      /* device_status only: a bounded device-side wait gave up */
+  KVC_ERR_TIMEOUT = -5,     /* device_status only: a bounded device-side wait gave up */
+  KVC_ERR_CAPACITY = -6     /* device_status only: rows did not fit in a cache (kvc_cache_gather, kvc_cache_append) */
 } kvc_status;
 
 typedef enum { KVC_F32 = 0, KVC_BF16 = 1 } kvc_dtype;
@@ -303,6 +304,138 @@ KVC_API kvc_status kvc_head_sum(const kvc_desc* desc, const float* scores, float
 KVC_API kvc_status kvc_add_head_mean(const kvc_desc* desc, float* scores, const float* head_sum,
                              int32_t n_kv_heads_total, void* stream);
 KVC_API kvc_status kvc_scale(float* x, int64_t n, float factor, void* stream);
+
+/*
+ * ---- decoding from a compressed cache ------------------------------------------------------------
+ * What follows the pass in a serving program: rotary positions for the queries and keys it scores and
+ * attends with (kvc_rotary), a cache held in 8 bits that takes the kept rows (kvc_cache_gather) and the
+ * rows of new tokens (kvc_cache_append), attention over it that adds up what every token was worth
+ * (kvc_attend), and eviction by that sum (kvc_evict).  One kvc_cache is one layer, or several layers of
+ * the same capacity laid out as one (layers times sequences as the batch): heads are independent.
+ */
+
+/* Rotary positions.  Pair i of a row at position p is turned by the angle p * f_i, i < rot_dim / 2:
+ *   y1 = m (x1 cos - x2 sin),  y2 = m (x2 cos + x1 sin)
+ * with (x1, x2) = (x[i], x[i + rot_dim / 2]), or (x[2i], x[2i + 1]) if interleaved; entries from rot_dim
+ * on are copied.  f_i = theta^(-2i / rot_dim), scaled for contexts beyond the original one:
+ *   KVC_ROPE_LINEAR  f_i / factor
+ *   KVC_ROPE_BANDED  by t_i = original_ctx f_i / 2pi, the pair's turns over the original context: f_i where
+ *                    t_i >= turns_high, f_i / factor where t_i <= turns_low, between them the two mixed
+ *                    linearly in t_i
+ *   KVC_ROPE_YARN    mixed linearly in i between the pairs that make turns_high and turns_low turns (rounded
+ *                    outwards, kept within [0, rot_dim - 1]); m = 0.1 ln(factor) + 1
+ * Angles are formed in 64 bits: at position 2^31 they are still within 1e-6. */
+typedef enum { KVC_ROPE_NONE = 0, KVC_ROPE_LINEAR = 1, KVC_ROPE_BANDED = 2, KVC_ROPE_YARN = 3 } kvc_rope_scaling;
+
+typedef struct {
+  int32_t batch, n_q_heads, n_kv_heads; /* q [batch, n_q_heads, rows, head_dim], k [batch, n_kv_heads, rows, head_dim] */
+  int32_t head_dim;                     /* 64 or 128 */
+  int32_t rows;                         /* >= 1 */
+  int32_t rot_dim;                      /* a multiple of 16, 16 <= rot_dim <= head_dim */
+  int32_t dtype;                        /* kvc_dtype of q, k and the outputs */
+  int32_t interleaved;                  /* 0: halves, 1: neighbours */
+  int32_t inverse;                      /* 1: turns by -p f_i (the gradient of the forward turn, as m stays) */
+  int32_t scaling;                      /* kvc_rope_scaling */
+  double theta;                         /* > 1 */
+  double factor;                        /* >= 1; used with scaling only, as are the three below */
+  double turns_low, turns_high;         /* 0 < turns_low < turns_high (BANDED, YARN) */
+  double original_ctx;                  /* > 0 (BANDED, YARN) */
+  double mscale;                        /* m; 0: as above (1 without YARN) */
+  int64_t q_stride[3], k_stride[3];     /* element strides (batch, head, row) of q, k, as in kvc_desc; 0 in slot 0: dense */
+  int64_t q_out_stride[3], k_out_stride[3];
+} kvc_rope_desc;
+
+/* positions: int64, position of row r of sequence b at [b * pos_stride + r] (pos_stride 0: the same for all
+ * sequences); may be negative.  q or k (with its output) may be NULL.  An output may be its input (same
+ * pointer and strides); other overlaps are not allowed. */
+KVC_API kvc_status kvc_rotary(const kvc_rope_desc* desc, const void* q, const void* k, const int64_t* positions,
+                              int64_t pos_stride, void* q_out, void* k_out, void* stream);
+
+/*
+ * A cache held in 8 bits.  `block` tokens of a head share an exponent, K and V apart: a value is
+ * code * 2^exponent.  With amax the largest magnitude in the block, the exponent is the smallest e with
+ * amax <= qmax * 2^e (qmax 127 for KVC_INT8, 448 for KVC_E4M3), within [-100, 121]; the code is
+ * value * 2^-e rounded to nearest, ties to even.  Powers of two: a value is rounded once, is exact in
+ * bf16, and keeps its code's digits when it moves to a block with another exponent, except where that is
+ * the larger one.  Rows behind a head's length are never read, and left as they are.
+ */
+typedef enum { KVC_INT8 = 0, KVC_E4M3 = 1 } kvc_cache_format;
+
+typedef struct {
+  int32_t batch, n_kv_heads; /* batch * n_kv_heads <= 65535 */
+  int32_t head_dim;          /* 64 or 128 */
+  int32_t block;             /* tokens per exponent: 16, 32, 64 or 128 */
+  int32_t format;            /* kvc_cache_format */
+  int32_t reserved_;         /* must be 0 */
+  int64_t capacity;          /* rows a head has room for, 1 <= capacity < 2^31 - 128 */
+  int64_t stride[3];         /* strides of k and v in codes (batch, head, token), multiples of 16; 0 in slot 0: dense */
+  void* k;                   /* [batch, n_kv_heads, capacity, head_dim], one byte per code; 16-byte aligned */
+  void* v;
+  int8_t* k_exp;             /* [batch, n_kv_heads, ceil(capacity / block)], dense */
+  int8_t* v_exp;
+  int32_t* lengths;          /* [batch, n_kv_heads]: rows in use, 0 .. capacity (others are taken as the nearer end) */
+} kvc_cache;
+
+/* kvc_gather into 8-bit caches, one per layer of desc: row i of head h of layer l becomes
+ * K[l][b, h, idx[l, b, h, i]] for i < n_keep, V alike, and lengths is set.  idx [L, batch, Hkv, N] may be NULL
+ * (row i is token i).  n_keep: [batch, L], or with per_head [batch, L, Hkv]; NULL keeps all N.  A layer that keeps
+ * more rows than its cache's capacity keeps the first ones, and *device_status (may be NULL; written only then)
+ * becomes KVC_ERR_CAPACITY.  An idx entry outside [0, N) gives a row of zeros.  caches: HOST array of L. */
+KVC_API kvc_status kvc_cache_gather(const kvc_desc* desc, const void* const* k, const void* const* v, const int32_t* idx,
+                                    const int32_t* n_keep, int32_t per_head, const kvc_cache* caches,
+                                    int32_t* device_status, void* stream);
+
+/* Rows of new tokens behind the ones in use.  k_new, v_new: [batch, Hkv, rows, head_dim] of kvc_dtype `dtype`, element
+ * strides `stride` (batch, head, row; NULL = dense).  n_new: [batch], rows that sequence b has of them (NULL: all;
+ * a padded batch).  The open block's exponent grows if the new rows need it (its codes are then rounded again), a
+ * block that starts takes the exponent of its rows.  lengths_out: the lengths afterwards, [batch, Hkv]; NULL writes
+ * them to cache->lengths.  weight (may be NULL): fp32 [batch, Hkv, capacity], set to 0 for the new rows.  Rows
+ * that do not fit are dropped, and *device_status (may be NULL; written only then) becomes KVC_ERR_CAPACITY. */
+KVC_API kvc_status kvc_cache_append(const kvc_cache* cache, const void* k_new, const void* v_new, int32_t dtype,
+                                    int32_t rows, const int64_t* stride, const int32_t* n_new, int32_t* lengths_out,
+                                    float* weight, int32_t* device_status, void* stream);
+
+/* Values back: k_out, v_out [batch, Hkv, rows, head_dim] of kvc_dtype `dtype`, dense, 16-byte aligned; row i is the
+ * cache's row first[b, h] + i (first NULL: 0), zeros where no such row is in use.  Either output may be NULL. */
+KVC_API kvc_status kvc_cache_read(const kvc_cache* cache, const int32_t* first, int64_t rows, int32_t dtype, void* k_out,
+                                  void* v_out, void* stream);
+
+/* Attention of a few query rows per sequence over an 8-bit cache. */
+typedef struct {
+  int32_t n_q_heads;     /* a multiple of the cache's n_kv_heads: query head j reads KV head j / (Hq / Hkv) */
+  int32_t rows;          /* query rows per sequence and head */
+  int32_t dtype;         /* kvc_dtype of q and out */
+  int32_t causal;        /* 1: the rows are the last tokens of the cache: of n rows, row m sees the first
+                            length - (n - 1 - m) tokens (none if that is < 1); 0: every row sees all */
+  float scale;           /* <= 0: 1 / sqrt(head_dim) */
+  int32_t reserved_;     /* must be 0 */
+  int64_t q_stride[3];   /* element strides (batch, head, row) of q, out, as in kvc_desc; 0 in slot 0: dense */
+  int64_t out_stride[3];
+} kvc_attend_desc;
+
+/* Bytes of scratch kvc_attend needs (host call); with_weight: with weight_out given. */
+KVC_API kvc_status kvc_attend_workspace_size(const kvc_cache* cache, const kvc_attend_desc* desc, int32_t with_weight,
+                                             size_t* bytes);
+
+/* out[b, j, m] = sum over the tokens c that row m sees of p[c] v[c], p = softmax over them of scale <q[b, j, m], k[c]>;
+ * a row that sees none gives zeros.  lse (may be NULL): [batch, Hq, rows] fp32, log of the softmax's denominator
+ * (natural; -inf for a row that sees none).  row_counts (may be NULL): [batch], rows that sequence b has (a padded
+ * batch); the others' outputs are left as they were, and they weigh nothing.  weight_out (may be NULL): fp32 [batch,
+ * Hkv, capacity]; weight_out[b, h, c] = weight_in[b, h, c] + sum of p[c] over the rows and the query heads of KV
+ * head h, for every c in use; weight_in may be weight_out, or NULL for zeros.  Sums are taken in a fixed order. */
+KVC_API kvc_status kvc_attend(const kvc_cache* cache, const kvc_attend_desc* desc, const void* q, const int32_t* row_counts,
+                              void* out, float* lse, const float* weight_in, float* weight_out, void* workspace,
+                              size_t workspace_bytes, void* stream);
+
+/* Eviction by accumulated weight, head by head: of the rows in use, the last `recent` and those with the largest weight
+ * among the others are kept, `budget` in all (all of them where no more are in use), in their order.  Equal weights
+ * keep the smaller position first.  The kept rows become dst's rows, weights go to weight_out [batch, Hkv,
+ * dst->capacity] (may be NULL), dst->lengths is set, and idx_out [batch, Hkv, budget] int32 holds the kept
+ * positions, then -1.  src and dst (same batch, heads, head_dim and format; not the same memory) may differ in block
+ * and capacity; 1 <= budget <= dst->capacity, 0 <= recent <= budget.  weight: fp32 [batch, Hkv, src->capacity],
+ * not NaN. */
+KVC_API kvc_status kvc_evict(const kvc_cache* src, const kvc_cache* dst, const float* weight, int64_t budget, int64_t recent,
+                             int32_t* idx_out, float* weight_out, void* stream);
 
 /* Message of the last error returned on this thread (static storage; never NULL). */
 KVC_API const char* kvc_last_error(void);

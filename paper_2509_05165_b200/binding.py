@@ -16,7 +16,7 @@ AGG_MAX, AGG_MEAN = 0, 1
 KVC_MAX_LAYERS = 128
 
 _STATUS = {0: "KVC_OK", -1: "KVC_ERR_INVALID_ARG", -2: "KVC_ERR_UNSUPPORTED", -3: "KVC_ERR_WORKSPACE",
-           -4: "KVC_ERR_CUDA", -5: "KVC_ERR_TIMEOUT"}
+           -4: "KVC_ERR_CUDA", -5: "KVC_ERR_TIMEOUT", -6: "KVC_ERR_CAPACITY"}
 
 
 class KvcError(RuntimeError):
@@ -35,6 +35,33 @@ class KvcDesc(C.Structure):
         ("q_stride", C.c_int64 * 3), ("kv_stride", C.c_int64 * 3),
         ("value_norm", C.c_int32), ("min_keep_per_layer", C.c_int32), ("keep_position_order", C.c_int32),
         ("reserved_", C.c_int32),
+    ]
+
+
+class KvcCache(C.Structure):
+    """``kvc_cache``: an 8-bit cache (see ``decode.Cache``)."""
+    _fields_ = [
+        ("batch", C.c_int32), ("n_kv_heads", C.c_int32), ("head_dim", C.c_int32), ("block", C.c_int32),
+        ("format", C.c_int32), ("reserved_", C.c_int32), ("capacity", C.c_int64), ("stride", C.c_int64 * 3),
+        ("k", C.c_void_p), ("v", C.c_void_p), ("k_exp", C.c_void_p), ("v_exp", C.c_void_p), ("lengths", C.c_void_p),
+    ]
+
+
+class KvcAttendDesc(C.Structure):
+    _fields_ = [
+        ("n_q_heads", C.c_int32), ("rows", C.c_int32), ("dtype", C.c_int32), ("causal", C.c_int32), ("scale", C.c_float),
+        ("reserved_", C.c_int32), ("q_stride", C.c_int64 * 3), ("out_stride", C.c_int64 * 3),
+    ]
+
+
+class KvcRopeDesc(C.Structure):
+    _fields_ = [
+        ("batch", C.c_int32), ("n_q_heads", C.c_int32), ("n_kv_heads", C.c_int32), ("head_dim", C.c_int32),
+        ("rows", C.c_int32), ("rot_dim", C.c_int32), ("dtype", C.c_int32), ("interleaved", C.c_int32),
+        ("inverse", C.c_int32), ("scaling", C.c_int32), ("theta", C.c_double), ("factor", C.c_double),
+        ("turns_low", C.c_double), ("turns_high", C.c_double), ("original_ctx", C.c_double), ("mscale", C.c_double),
+        ("q_stride", C.c_int64 * 3), ("k_stride", C.c_int64 * 3), ("q_out_stride", C.c_int64 * 3),
+        ("k_out_stride", C.c_int64 * 3),
     ]
 
 
@@ -105,6 +132,16 @@ def _load():
     lib.kvc_gather.restype = C.c_int
     lib.kvc_compress.argtypes = [dp, vp, vp, vp, i64, vp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
     lib.kvc_compress.restype = C.c_int
+    cp, ap = C.POINTER(KvcCache), C.POINTER(KvcAttendDesc)
+    lib.kvc_rotary.argtypes = [C.POINTER(KvcRopeDesc), vp, vp, vp, i64, vp, vp, vp]
+    lib.kvc_cache_gather.argtypes = [dp, vp, vp, vp, vp, i32, cp, vp, vp]
+    lib.kvc_cache_append.argtypes = [cp, vp, vp, i32, i32, C.POINTER(i64), vp, vp, vp, vp, vp]
+    lib.kvc_cache_read.argtypes = [cp, vp, i64, i32, vp, vp, vp]
+    lib.kvc_attend_workspace_size.argtypes = [cp, ap, i32, C.POINTER(sz)]
+    lib.kvc_attend.argtypes = [cp, ap, vp, vp, vp, vp, vp, vp, vp, sz, vp]
+    lib.kvc_evict.argtypes = [cp, cp, vp, i64, i64, vp, vp, vp]
+    for name in ("rotary", "cache_gather", "cache_append", "cache_read", "attend_workspace_size", "attend", "evict"):
+        getattr(lib, "kvc_" + name).restype = C.c_int
     lib.kvc_last_error.restype = C.c_char_p
     lib.kvc_launch_count.argtypes = [i32]
     lib.kvc_launch_count.restype = i64

@@ -1,0 +1,416 @@
+// The 8-bit cache (kvc.h): taking kept rows in (kvc_cache_gather), new tokens (kvc_cache_append), values back
+// (kvc_cache_read).
+//
+// The unit of work is a block of tokens of one head, K or V: its exponent needs the largest of its block * d values before
+// the first code can be rounded, so a job of block * d / 32 threads holds the block in registers, 32 values per thread,
+// reduces the maximum once and writes codes.  Every source row is read once and every code written once; HBM is the bound.
+#include "cache8.cuh"
+
+namespace kvc {
+namespace {
+
+// ---- kept rows of a prefilled cache -----------------------------------------------------------------------------------
+
+struct GatherLayer {
+  const void *k, *v;
+  uint8_t *ko, *vo;
+  int8_t *ke, *ve;
+  int32_t* lengths;
+  long long cap, blocks, st[3];
+};
+
+struct CacheGatherParams {
+  int L, Bt, Hkv, d, block_shift, per_head;
+  long long N, kvs[3];
+  GatherLayer layer[KVC_MAX_LAYERS];
+};
+
+template <typename T, int kFormat>
+__global__ void __launch_bounds__(512)
+cache_gather_kernel(const __grid_constant__ CacheGatherParams P, const int32_t* __restrict__ idx,
+                    const int32_t* __restrict__ n_keep, int32_t* device_status) {
+  __shared__ float scratch[16];
+  grid_dependency_wait();
+  const int l = blockIdx.z >> 1, is_v = blockIdx.z & 1;
+  const int unit = blockIdx.y, b = unit / P.Hkv, h = unit - b * P.Hkv;
+  const GatherLayer& y = P.layer[l];
+  long long n = P.N;
+  if (n_keep != nullptr) {
+    n = P.per_head ? n_keep[((long long)b * P.L + l) * P.Hkv + h] : n_keep[(long long)b * P.L + l];
+    n = n < 0 ? 0 : (n > P.N ? P.N : n);
+  }
+  if (blockIdx.x == 0 && is_v == 0 && threadIdx.x == 0) {
+    y.lengths[unit] = (int32_t)(n < y.cap ? n : y.cap);
+    if (n > y.cap && device_status != nullptr) *device_status = KVC_ERR_CAPACITY;
+  }
+  if (n > y.cap) n = y.cap;
+
+  const JobLane j(P.block_shift, P.d);
+  const long long blk = (long long)blockIdx.x * (blockDim.x / j.threads) + j.slot;
+  const long long row0 = blk << P.block_shift;
+  if (((long long)blockIdx.x * (blockDim.x / j.threads) << P.block_shift) >= n) return;    // (the whole CTA)
+  const T* src = reinterpret_cast<const T*>(is_v ? y.v : y.k) + b * P.kvs[0] + h * P.kvs[1];
+  const int32_t* map = idx == nullptr ? nullptr : idx + (((long long)l * P.Bt + b) * P.Hkv + h) * P.N;
+  float x[4][8];
+  float top = 0.f;
+  long long at[4];
+#pragma unroll
+  for (int g = 0; g < 4; ++g) {
+    const long long r = row0 + j.row(g);
+    at[g] = -1;
+    if (r < n) {
+      at[g] = map == nullptr ? r : map[r];
+      if (at[g] >= P.N) at[g] = -1;
+    }
+  }
+#pragma unroll
+  for (int g = 0; g < 4; ++g) {
+    if (at[g] >= 0) {
+      load8<T>(src + at[g] * P.kvs[2] + j.col(g), x[g]);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) x[g][i] = 0.f;
+    }
+  }
+#pragma unroll
+  for (int g = 0; g < 4; ++g)
+#pragma unroll
+    for (int i = 0; i < 8; ++i) top = fmaxf(top, fabsf(x[g][i]));
+  const int e = exponent_of<kFormat>(job_max(top, j, scratch));
+  if (row0 >= n) return;
+  const float f = pow2(-e);
+  uint8_t* out = (is_v ? y.vo : y.ko) + b * y.st[0] + h * y.st[1];
+#pragma unroll
+  for (int g = 0; g < 4; ++g) {
+    const long long r = row0 + j.row(g);
+    if (r < n)
+      *reinterpret_cast<uint2*>(out + r * y.st[2] + j.col(g)) =
+          make_uint2(encode4<kFormat>(x[g][0], x[g][1], x[g][2], x[g][3], f), encode4<kFormat>(x[g][4], x[g][5], x[g][6], x[g][7], f));
+  }
+  if (j.t == 0) (is_v ? y.ve : y.ke)[(long long)unit * y.blocks + blk] = (int8_t)e;
+}
+
+// ---- new tokens -------------------------------------------------------------------------------------------------------
+
+struct AppendParams {
+  Cache c;
+  int rows, jobs_per_cta;                // jobs_per_cta: blocks (of K and of V) that a CTA takes, per grid step
+  long long ns[3];
+  bool write_lengths;                    // the lengths are written here (else by append_lengths_kernel)
+};
+
+__device__ __forceinline__ int rows_of(const AppendParams& P, const int32_t* n_new, int b) {
+  const int n = n_new == nullptr ? P.rows : n_new[b];
+  return n < 0 ? 0 : (n > P.rows ? P.rows : n);
+}
+
+// A CTA takes blocks blockIdx.x * jobs_per_cta .. of the ones that a head's new rows touch, counted from its open block.
+template <typename T, int kFormat>
+__global__ void __launch_bounds__(512)
+cache_append_kernel(const __grid_constant__ AppendParams P, const T* __restrict__ k_new, const T* __restrict__ v_new,
+                    const int32_t* __restrict__ n_new, int32_t* lengths_out, float* __restrict__ weight, int32_t* device_status) {
+  __shared__ float scratch[16];
+  grid_dependency_wait();
+  const Cache& c = P.c;
+  const int unit = blockIdx.y, b = unit / c.Hkv, h = unit - b * c.Hkv;
+  const long long len = c.length(unit);
+  const int want = rows_of(P, n_new, b);
+  const int n = (int)(want < c.cap - len ? want : c.cap - len);
+  __syncthreads();                       // every thread has the length before it may change
+  if (blockIdx.x == 0 && threadIdx.x == 0) {
+    if (P.write_lengths) lengths_out[unit] = (int32_t)(len + n);
+    if (n < want && device_status != nullptr) *device_status = KVC_ERR_CAPACITY;
+  }
+  if (n == 0) return;
+  const JobLane j(c.block_shift, c.d);
+  const int slots = blockDim.x / j.threads;
+  const long long blk0 = len >> c.block_shift;
+  const int touched = (int)(((len + n - 1) >> c.block_shift) - blk0) + 1;
+  const int first = blockIdx.x * P.jobs_per_cta, last = min(first + P.jobs_per_cta, touched);
+  // jobs: block `first`'s K and V, the next block's, ...
+  for (int jb = 2 * first; jb < 2 * last; jb += slots) {
+    const int job = jb + j.slot;
+    const bool live = job < 2 * last;
+    const int is_v = job & 1;
+    const long long blk = blk0 + (job >> 1), row0 = blk << c.block_shift;
+    uint8_t* codes = (is_v ? c.v : c.k) + c.base(unit);
+    int8_t* exps = (is_v ? c.v_exp : c.k_exp) + (long long)unit * c.blocks;
+    const T* src = (is_v ? v_new : k_new) + b * P.ns[0] + h * P.ns[1];
+    float x[4][8];
+    float top = 0.f;
+#pragma unroll
+    for (int g = 0; g < 4; ++g) {
+      const long long r = row0 + j.row(g) - len;          // the row's number among the new ones
+      if (live && r >= 0 && r < n) {
+        load8<T>(src + r * P.ns[2] + j.col(g), x[g]);
+        if (weight != nullptr && is_v == 0 && j.col(g) == 0) weight[unit * c.cap + len + r] = 0.f;
+      } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[g][i] = 0.f;
+      }
+#pragma unroll
+      for (int i = 0; i < 8; ++i) top = fmaxf(top, fabsf(x[g][i]));
+    }
+    int e = exponent_of<kFormat>(job_max(top, j, scratch));
+    if (!live) continue;
+    if (row0 < len) {                                     // the open block has rows already
+      const int was = exps[blk];
+      e = max(e, was);
+      if (e > was) {
+        const float f = pow2_clamped(was - e);
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+          if (row0 + j.row(g) < len) {
+            uint2* p = reinterpret_cast<uint2*>(codes + (row0 + j.row(g)) * c.st[2] + j.col(g));
+            const uint2 w = *p;
+            float y[8];
+            decode4<kFormat>(w.x, y);
+            decode4<kFormat>(w.y, y + 4);
+            *p = make_uint2(encode4<kFormat>(y[0], y[1], y[2], y[3], f), encode4<kFormat>(y[4], y[5], y[6], y[7], f));
+          }
+        }
+      }
+    }
+    const float f = pow2(-e);
+#pragma unroll
+    for (int g = 0; g < 4; ++g) {
+      const long long r = row0 + j.row(g);
+      if (r >= len && r < len + n)
+        *reinterpret_cast<uint2*>(codes + r * c.st[2] + j.col(g)) =
+            make_uint2(encode4<kFormat>(x[g][0], x[g][1], x[g][2], x[g][3], f), encode4<kFormat>(x[g][4], x[g][5], x[g][6], x[g][7], f));
+    }
+    // every thread of the job has read the old exponent before it changes
+    if (j.threads == 32) __syncwarp(); else asm volatile("bar.sync %0, %1;" :: "r"(1 + j.slot), "r"(j.threads) : "memory");
+    if (j.t == 0) exps[blk] = (int8_t)e;
+  }
+}
+
+__global__ void append_lengths_kernel(const __grid_constant__ AppendParams P, const int32_t* __restrict__ n_new, int32_t* lengths_out) {
+  grid_dependency_wait();
+  const int unit = blockIdx.x * blockDim.x + threadIdx.x;
+  if (unit >= P.c.units()) return;
+  const long long len = P.c.length(unit), want = rows_of(P, n_new, unit / P.c.Hkv);
+  lengths_out[unit] = (int32_t)(len + (want < P.c.cap - len ? want : P.c.cap - len));
+}
+
+// ---- values back ------------------------------------------------------------------------------------------------------
+
+struct ReadParams {
+  Cache c;
+  long long rows;
+};
+
+template <typename T, int kFormat>
+__global__ void __launch_bounds__(256)
+cache_read_kernel(const __grid_constant__ ReadParams P, const int32_t* __restrict__ first, T* __restrict__ k_out, T* __restrict__ v_out) {
+  grid_dependency_wait();
+  const Cache& c = P.c;
+  const int unit = blockIdx.y;
+  const bool is_v = k_out == nullptr || blockIdx.z == 1;
+  const int shift = c.d == 128 ? 3 : 2;                   // log2(d / 16)
+  const long long len = c.length(unit), row_first = first == nullptr ? 0 : first[unit];
+  const uint8_t* codes = (is_v ? c.v : c.k) + c.base(unit);
+  const int8_t* exps = (is_v ? c.v_exp : c.k_exp) + (long long)unit * c.blocks;
+  T* out = (is_v ? v_out : k_out) + unit * P.rows * c.d;
+  const long long total = P.rows << shift;
+  for (long long i = (long long)blockIdx.x * blockDim.x + threadIdx.x; i < total; i += (long long)gridDim.x * blockDim.x) {
+    const long long r = row_first + (i >> shift);
+    const int col = (int)(i & ((1 << shift) - 1)) * 16;
+    uint4 w = make_uint4(0, 0, 0, 0);
+    float f = 0.f;
+    if (r >= 0 && r < len) {
+      w = ld16_stream(codes + r * c.st[2] + col);
+      f = pow2_clamped(exps[r >> c.block_shift]);
+    }
+    float x[16];
+    decode4<kFormat>(w.x, x); decode4<kFormat>(w.y, x + 4); decode4<kFormat>(w.z, x + 8); decode4<kFormat>(w.w, x + 12);
+    T* o = out + (i << 4);
+    if (sizeof(T) == 2) {
+      uint32_t u[8];
+#pragma unroll
+      for (int q = 0; q < 8; ++q) {
+        const __nv_bfloat162 t = __floats2bfloat162_rn(x[2 * q] * f, x[2 * q + 1] * f);
+        u[q] = *reinterpret_cast<const uint32_t*>(&t);
+      }
+      reinterpret_cast<uint4*>(o)[0] = make_uint4(u[0], u[1], u[2], u[3]);
+      reinterpret_cast<uint4*>(o)[1] = make_uint4(u[4], u[5], u[6], u[7]);
+    } else {
+#pragma unroll
+      for (int q = 0; q < 4; ++q)
+        reinterpret_cast<float4*>(o)[q] = make_float4(x[4 * q] * f, x[4 * q + 1] * f, x[4 * q + 2] * f, x[4 * q + 3] * f);
+    }
+  }
+}
+
+template <typename T>
+kvc_status run_gather(const CacheGatherParams& P, int format, int block, long long most_cap, const int32_t* idx, const int32_t* n_keep,
+                      int32_t* status, cudaStream_t st) {
+  const int job = block * P.d / 32, threads = job > 256 ? job : 256;
+  const long long rows = most_cap < P.N ? most_cap : P.N, per_cta = (long long)(threads / job) * block;
+  const dim3 grid((unsigned)((rows + per_cta - 1) / per_cta), P.Bt * P.Hkv, 2 * P.L);
+  auto kernel = format == KVC_E4M3 ? cache_gather_kernel<T, KVC_E4M3> : cache_gather_kernel<T, KVC_INT8>;
+  KVC_CUDA(launch_dependent(kernel, grid, dim3(threads), 0, st, P, idx, n_keep, status));
+  KVC_LAUNCH_CHECK("cache_gather_kernel");
+  return KVC_OK;
+}
+
+}  // namespace
+
+bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
+
+kvc_status check_dtype(int32_t dtype) {
+  KVC_REQUIRE8(dtype == KVC_F32 || dtype == KVC_BF16, KVC_ERR_INVALID_ARG, "unknown dtype");
+  return KVC_OK;
+}
+
+kvc_status resolve_strides(const int64_t* given, int batch, int heads, long long rows, int d, int elem_bytes, bool written,
+                           const char* name, long long* out) {
+  if (given == nullptr || given[0] == 0) {
+    out[2] = d; out[1] = rows * d; out[0] = out[1] * heads;
+    return KVC_OK;
+  }
+  for (int i = 0; i < 3; ++i) {
+    KVC_REQUIRE8(given[i] >= (i == 2 ? d : 0) && given[i] % (16 / elem_bytes) == 0, KVC_ERR_INVALID_ARG,
+                 "%s[%d] must be a non-negative multiple of 16 bytes (rows >= head_dim apart)", name, i);
+    out[i] = given[i];
+  }
+  if (!written) return KVC_OK;
+  // dimensions from the narrowest on: each must step over all that the narrower ones span
+  const long long size[3] = {batch, heads, rows};
+  int order[3] = {0, 1, 2};
+  for (int i = 0; i < 2; ++i)
+    for (int k = i + 1; k < 3; ++k)
+      if (out[order[k]] < out[order[i]]) { const int t = order[i]; order[i] = order[k]; order[k] = t; }
+  long long extent = d;
+  for (int i : order) {
+    if (size[i] <= 1) continue;
+    KVC_REQUIRE8(out[i] >= extent, KVC_ERR_INVALID_ARG, "%s: rows of an array that is written to overlap", name);
+    extent += out[i] * (size[i] - 1);
+  }
+  return KVC_OK;
+}
+
+kvc_status resolve_cache(const kvc_cache* c, const char* name, Cache* out) {
+  KVC_REQUIRE8(c != nullptr, KVC_ERR_INVALID_ARG, "%s is NULL", name);
+  KVC_REQUIRE8(c->batch >= 1 && c->n_kv_heads >= 1, KVC_ERR_INVALID_ARG, "%s: batch and n_kv_heads must be >= 1", name);
+  KVC_REQUIRE8((long long)c->batch * c->n_kv_heads <= 65535, KVC_ERR_UNSUPPORTED, "%s: batch * n_kv_heads > 65535", name);
+  KVC_REQUIRE8(c->head_dim == 64 || c->head_dim == 128, KVC_ERR_UNSUPPORTED, "%s: head_dim must be 64 or 128", name);
+  KVC_REQUIRE8(c->block == 16 || c->block == 32 || c->block == 64 || c->block == 128, KVC_ERR_UNSUPPORTED,
+               "%s: block must be 16, 32, 64 or 128", name);
+  KVC_REQUIRE8(c->format == KVC_INT8 || c->format == KVC_E4M3, KVC_ERR_INVALID_ARG, "%s: unknown format", name);
+  KVC_REQUIRE8(c->reserved_ == 0, KVC_ERR_INVALID_ARG, "%s: reserved_ must be 0", name);
+  KVC_REQUIRE8(c->capacity >= 1, KVC_ERR_INVALID_ARG, "%s: capacity must be >= 1", name);
+  KVC_REQUIRE8(c->capacity < (1LL << 31) - 128, KVC_ERR_UNSUPPORTED, "%s: capacity must be < 2^31 - 128", name);
+  KVC_REQUIRE8(c->k && c->v && c->k_exp && c->v_exp && c->lengths, KVC_ERR_INVALID_ARG, "%s: k, v, k_exp, v_exp or lengths is NULL", name);
+  KVC_REQUIRE8(aligned16(c->k) && aligned16(c->v), KVC_ERR_INVALID_ARG, "%s: k or v is not 16-byte aligned", name);
+  KVC_REQUIRE8((reinterpret_cast<uintptr_t>(c->lengths) & 3u) == 0, KVC_ERR_INVALID_ARG, "%s: lengths is not 4-byte aligned", name);
+  out->Bt = c->batch; out->Hkv = c->n_kv_heads; out->d = c->head_dim; out->block = c->block; out->format = c->format;
+  out->block_shift = c->block == 16 ? 4 : c->block == 32 ? 5 : c->block == 64 ? 6 : 7;
+  out->cap = c->capacity;
+  out->blocks = (c->capacity + c->block - 1) / c->block;
+  out->k = (uint8_t*)c->k; out->v = (uint8_t*)c->v; out->k_exp = c->k_exp; out->v_exp = c->v_exp; out->lengths = c->lengths;
+  return resolve_strides(c->stride, c->batch, c->n_kv_heads, c->capacity, c->head_dim, 1, true, name, out->st);
+}
+
+}  // namespace kvc
+
+using namespace kvc;
+
+extern "C" {
+
+kvc_status kvc_cache_gather(const kvc_desc* d, const void* const* k, const void* const* v, const int32_t* idx, const int32_t* n_keep,
+                            int32_t per_head, const kvc_cache* caches, int32_t* device_status, void* stream) {
+  Problem P;
+  kvc_status s = resolve_desc(d, &P);
+  if (s != KVC_OK) return s;
+  KVC_REQUIRE8(k != nullptr && v != nullptr, KVC_ERR_INVALID_ARG, "k or v pointer array is NULL");
+  KVC_REQUIRE8(caches != nullptr, KVC_ERR_INVALID_ARG, "caches is NULL");
+  KVC_REQUIRE8(per_head == 0 || per_head == 1, KVC_ERR_INVALID_ARG, "per_head must be 0 or 1");
+  KVC_REQUIRE8((long long)P.Bt * P.Hkv <= 65535, KVC_ERR_UNSUPPORTED, "batch * n_kv_heads > 65535");
+  CacheGatherParams gp;
+  gp.L = P.L; gp.Bt = P.Bt; gp.Hkv = P.Hkv; gp.d = P.d; gp.per_head = per_head; gp.N = P.N;
+  for (int i = 0; i < 3; ++i) gp.kvs[i] = P.kvs[i];
+  long long most = 0;
+  for (int l = 0; l < P.L; ++l) {
+    Cache c;
+    if ((s = resolve_cache(caches + l, "caches", &c)) != KVC_OK) return s;
+    KVC_REQUIRE8(c.Bt == P.Bt && c.Hkv == P.Hkv && c.d == P.d, KVC_ERR_INVALID_ARG, "caches[%d] has another batch, head count or head_dim than desc", l);
+    KVC_REQUIRE8(c.block == caches[0].block && c.format == caches[0].format, KVC_ERR_INVALID_ARG,
+                 "caches[%d] has another block or format than caches[0]", l);
+    KVC_REQUIRE8(k[l] && v[l] && aligned16(k[l]) && aligned16(v[l]), KVC_ERR_INVALID_ARG, "k[%d] or v[%d] is NULL or not 16-byte aligned", l, l);
+    gp.block_shift = c.block_shift;
+    gp.layer[l] = GatherLayer{k[l], v[l], c.k, c.v, c.k_exp, c.v_exp, c.lengths, c.cap, c.blocks, {c.st[0], c.st[1], c.st[2]}};
+    if (c.cap > most) most = c.cap;
+  }
+  if ((s = require_device()) != KVC_OK) return s;
+  return P.dtype == KVC_F32
+             ? run_gather<float>(gp, caches[0].format, caches[0].block, most, idx, n_keep, device_status, (cudaStream_t)stream)
+             : run_gather<__nv_bfloat16>(gp, caches[0].format, caches[0].block, most, idx, n_keep, device_status, (cudaStream_t)stream);
+}
+
+kvc_status kvc_cache_append(const kvc_cache* cache, const void* k_new, const void* v_new, int32_t dtype, int32_t rows,
+                            const int64_t* stride, const int32_t* n_new, int32_t* lengths_out, float* weight,
+                            int32_t* device_status, void* stream) {
+  AppendParams P;
+  kvc_status s = resolve_cache(cache, "cache", &P.c);
+  if (s != KVC_OK) return s;
+  if ((s = check_dtype(dtype)) != KVC_OK) return s;
+  KVC_REQUIRE8(k_new && v_new && aligned16(k_new) && aligned16(v_new), KVC_ERR_INVALID_ARG, "k_new or v_new is NULL or not 16-byte aligned");
+  KVC_REQUIRE8(rows >= 1, KVC_ERR_INVALID_ARG, "rows must be >= 1");
+  KVC_REQUIRE8(rows <= (1 << 30), KVC_ERR_UNSUPPORTED, "rows > 2^30");
+  if ((s = resolve_strides(stride, P.c.Bt, P.c.Hkv, rows, P.c.d, dtype == KVC_F32 ? 4 : 2, false, "stride", P.ns)) != KVC_OK) return s;
+  if ((s = require_device()) != KVC_OK) return s;
+  P.rows = rows;
+  if (lengths_out == nullptr) lengths_out = P.c.lengths;
+  // (a head's new rows touch at most this many blocks, wherever its open block ends)
+  const long long touched = ((long long)rows + P.c.block - 2) / P.c.block + 1;
+  // up to four blocks: one CTA per head, which can then write the length itself; more: a CTA per block
+  P.jobs_per_cta = touched <= 4 ? (int)touched : 1;
+  const long long steps = (touched + P.jobs_per_cta - 1) / P.jobs_per_cta;
+  P.write_lengths = steps == 1 || lengths_out != P.c.lengths;
+  const dim3 grid((unsigned)steps, P.c.units()), threads(job_cta_threads(P.c));
+  const bool e4m3 = P.c.format == KVC_E4M3;
+  cudaStream_t st = (cudaStream_t)stream;
+  if (dtype == KVC_F32)
+    KVC_CUDA(launch_dependent(e4m3 ? cache_append_kernel<float, KVC_E4M3> : cache_append_kernel<float, KVC_INT8>, grid, threads, 0, st, P,
+                              (const float*)k_new, (const float*)v_new, n_new, lengths_out, weight, device_status));
+  else
+    KVC_CUDA(launch_dependent(e4m3 ? cache_append_kernel<__nv_bfloat16, KVC_E4M3> : cache_append_kernel<__nv_bfloat16, KVC_INT8>, grid,
+                              threads, 0, st, P, (const __nv_bfloat16*)k_new, (const __nv_bfloat16*)v_new, n_new, lengths_out, weight,
+                              device_status));
+  KVC_LAUNCH_CHECK("cache_append_kernel");
+  if (!P.write_lengths) {
+    KVC_CUDA(launch_dependent(append_lengths_kernel, dim3((P.c.units() + 127) / 128), dim3(128), 0, st, P, n_new, lengths_out));
+    KVC_LAUNCH_CHECK("append_lengths_kernel");
+  }
+  return KVC_OK;
+}
+
+kvc_status kvc_cache_read(const kvc_cache* cache, const int32_t* first, int64_t rows, int32_t dtype, void* k_out, void* v_out, void* stream) {
+  ReadParams P;
+  kvc_status s = resolve_cache(cache, "cache", &P.c);
+  if (s != KVC_OK) return s;
+  if ((s = check_dtype(dtype)) != KVC_OK) return s;
+  KVC_REQUIRE8(k_out != nullptr || v_out != nullptr, KVC_ERR_INVALID_ARG, "k_out and v_out are both NULL");
+  KVC_REQUIRE8(aligned16(k_out) && aligned16(v_out), KVC_ERR_INVALID_ARG, "k_out or v_out is not 16-byte aligned");
+  KVC_REQUIRE8(rows >= 1, KVC_ERR_INVALID_ARG, "rows must be >= 1");
+  KVC_REQUIRE8(rows < (1LL << 31), KVC_ERR_UNSUPPORTED, "rows must be < 2^31");
+  if ((s = require_device()) != KVC_OK) return s;
+  P.rows = rows;
+  const long long items = rows * P.c.d / 16;
+  long long ctas = (items + 255) / 256;
+  if (ctas > 65536) ctas = 65536;
+  const dim3 grid((unsigned)ctas, P.c.units(), k_out != nullptr && v_out != nullptr ? 2 : 1);
+  const bool e4m3 = P.c.format == KVC_E4M3;
+  cudaStream_t st = (cudaStream_t)stream;
+  if (dtype == KVC_F32)
+    KVC_CUDA(launch_dependent(e4m3 ? cache_read_kernel<float, KVC_E4M3> : cache_read_kernel<float, KVC_INT8>, grid, dim3(256), 0, st, P,
+                              first, (float*)k_out, (float*)v_out));
+  else
+    KVC_CUDA(launch_dependent(e4m3 ? cache_read_kernel<__nv_bfloat16, KVC_E4M3> : cache_read_kernel<__nv_bfloat16, KVC_INT8>, grid,
+                              dim3(256), 0, st, P, first, (__nv_bfloat16*)k_out, (__nv_bfloat16*)v_out));
+  KVC_LAUNCH_CHECK("cache_read_kernel");
+  return KVC_OK;
+}
+
+}  // extern "C"

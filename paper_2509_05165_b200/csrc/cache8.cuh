@@ -1,0 +1,155 @@
+// The 8-bit cache of kvc.h: resolved descriptor, exponents and codes.  Shared by cache8.cu, evict.cu and attend.cu.
+#pragma once
+
+#include <cuda_fp8.h>
+
+#include "kvc_internal.cuh"
+
+namespace kvc {
+
+constexpr int kExpMin = -100, kExpMax = 121;   // 2^e and 2^-e are normal fp32 numbers with room for the codes
+
+// A kvc_cache with its strides filled in.
+struct Cache {
+  int Bt, Hkv, d, block, block_shift, format;
+  long long cap, blocks;                  // blocks: exponents per head
+  long long st[3];                        // in codes (bytes)
+  uint8_t *k, *v;
+  int8_t *k_exp, *v_exp;
+  int32_t* lengths;
+  __host__ __device__ int units() const { return Bt * Hkv; }
+  __device__ __forceinline__ long long base(int unit) const { return (unit / Hkv) * st[0] + (unit % Hkv) * st[1]; }
+  // rows in use, whatever the caller's array holds
+  __device__ __forceinline__ long long length(int unit) const {
+    const long long n = lengths[unit];
+    return n < 0 ? 0 : (n > cap ? cap : n);
+  }
+};
+
+kvc_status resolve_cache(const kvc_cache* c, const char* name, Cache* out);
+// Element strides (batch, head, row) of a [batch, heads, rows, d] array: checked, or dense.  An array that is written to
+// must not overlap itself.
+kvc_status resolve_strides(const int64_t* given, int batch, int heads, long long rows, int d, int elem_bytes, bool written,
+                           const char* name, long long* out);
+// kvc_dtype of an argument that is not part of a kvc_desc.
+kvc_status check_dtype(int32_t dtype);
+bool aligned16(const void* p);
+
+#define KVC_REQUIRE8(cond, code, ...)     \
+  do {                                    \
+    if (!(cond)) {                        \
+      ::kvc::set_error(__VA_ARGS__);      \
+      return code;                        \
+    }                                     \
+  } while (0)
+
+#ifdef __CUDACC__
+
+// 2^e for e in [-126, 127]
+__device__ __forceinline__ float pow2(int e) { return __int_as_float((e + 127) << 23); }
+__device__ __forceinline__ float pow2_clamped(int e) { return pow2(min(max(e, -126), 127)); }
+
+// The smallest e with amax <= qmax 2^e: with amax = m 2^E, m in [1, 2), that is E minus the exponent of qmax, and one
+// more where m exceeds qmax's own significand (448 = 1.75 * 2^8, 127 = 1.984375 * 2^6).  Zero and subnormal amax end at
+// the lower bound, infinity at the upper one.
+template <int kFormat>
+__device__ __forceinline__ int exponent_of(float amax) {
+  const uint32_t b = __float_as_uint(amax);
+  const int E = (int)(b >> 23) - 127;
+  const uint32_t m = b & 0x7fffffu;
+  const int e = kFormat == KVC_E4M3 ? E - 8 + (m > 0x600000u) : E - 6 + (m > 0x7e0000u);
+  return min(max(e, kExpMin), kExpMax);
+}
+
+// Codes of four values x * f (f a power of two, so the product is exact but for what rounds to zero): rounded to
+// nearest, ties to even, held at the largest code.
+template <int kFormat>
+__device__ __forceinline__ uint32_t encode4(float x0, float x1, float x2, float x3, float f) {
+  if (kFormat == KVC_E4M3) {
+    uint16_t lo, hi;
+    asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(lo) : "f"(x1 * f), "f"(x0 * f));
+    asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(hi) : "f"(x3 * f), "f"(x2 * f));
+    return (uint32_t)lo | ((uint32_t)hi << 16);
+  }
+  const int a = min(max(__float2int_rn(x0 * f), -127), 127), b = min(max(__float2int_rn(x1 * f), -127), 127);
+  const int c = min(max(__float2int_rn(x2 * f), -127), 127), d = min(max(__float2int_rn(x3 * f), -127), 127);
+  return (a & 255) | ((b & 255) << 8) | ((c & 255) << 16) | ((uint32_t)d << 24);
+}
+
+// The values of four codes, without the exponent.
+template <int kFormat>
+__device__ __forceinline__ void decode4(uint32_t w, float* x) {
+  if (kFormat == KVC_E4M3) {
+    uint32_t a, b;
+    asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(a) : "h"((uint16_t)w));
+    asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(b) : "h"((uint16_t)(w >> 16)));
+    const float2 fa = __half22float2(*reinterpret_cast<__half2*>(&a)), fb = __half22float2(*reinterpret_cast<__half2*>(&b));
+    x[0] = fa.x; x[1] = fa.y; x[2] = fb.x; x[3] = fb.y;
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x[i] = (float)(int8_t)(w >> (8 * i));
+  }
+}
+
+__device__ __forceinline__ uint4 ld16(const void* p) { return *reinterpret_cast<const uint4*>(p); }
+__device__ __forceinline__ uint4 ld16_stream(const void* p) {
+  uint4 v;
+  asm volatile("ld.global.nc.L1::no_allocate.v4.u32 {%0,%1,%2,%3}, [%4];"
+               : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p));
+  return v;
+}
+
+// A block's tokens as one job of block * d / 32 threads with 32 values each, four groups of eight: kFirst .. of a row.
+// The jobs of a CTA lie side by side; a job is one warp or whole warps.
+struct JobLane {
+  int threads, slot, t, per_row_shift;    // per_row_shift: log2(d / 8)
+  __device__ __forceinline__ JobLane(int block_shift, int d) {
+    per_row_shift = d == 128 ? 4 : 3;
+    threads = 1 << (block_shift + per_row_shift - 2);
+    slot = threadIdx.x / threads;
+    t = threadIdx.x - slot * threads;
+  }
+  __device__ __forceinline__ int row(int g) const { return (g * threads + t) >> per_row_shift; }
+  __device__ __forceinline__ int col(int g) const { return ((g * threads + t) & ((1 << per_row_shift) - 1)) * 8; }
+};
+
+// The largest of a job's threads' values; every thread of the CTA calls it.  scratch: one float per warp.
+__device__ __forceinline__ float job_max(float x, const JobLane& j, float* scratch) {
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, o));
+  if (j.threads == 32) return x;
+  __syncthreads();                        // (the scratch of the call before has been read)
+  if ((threadIdx.x & 31) == 0) scratch[threadIdx.x >> 5] = x;
+  __syncthreads();
+  const int w0 = j.slot * (j.threads >> 5);
+  x = scratch[w0];
+  for (int i = 1; i < (j.threads >> 5); ++i) x = fmaxf(x, scratch[w0 + i]);
+  return x;
+}
+
+template <typename T>
+__device__ __forceinline__ void load8(const T* p, float* x) {
+  if (sizeof(T) == 2) {
+    const uint4 w = ld16_stream(p);
+    const uint32_t u[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      x[2 * i] = __uint_as_float(u[i] << 16);
+      x[2 * i + 1] = __uint_as_float(u[i] & 0xffff0000u);
+    }
+  } else {
+    const uint4 a = ld16_stream(p), b = ld16_stream(p + 4);
+    x[0] = __uint_as_float(a.x); x[1] = __uint_as_float(a.y); x[2] = __uint_as_float(a.z); x[3] = __uint_as_float(a.w);
+    x[4] = __uint_as_float(b.x); x[5] = __uint_as_float(b.y); x[6] = __uint_as_float(b.z); x[7] = __uint_as_float(b.w);
+  }
+}
+
+// Threads of a CTA that works on blocks: at least 256, and whole jobs.
+inline int job_cta_threads(const Cache& c) {
+  const int t = c.block * c.d / 32;
+  return t > 256 ? t : 256;
+}
+
+#endif  // __CUDACC__
+
+}  // namespace kvc

@@ -1,0 +1,273 @@
+"""Decoding from a compressed cache: the binding of kvc.h's 8-bit cache, its attention and eviction, and rotary positions.
+
+Same names as the C entry points; tensors are checked for type, shape, layout and device here, values and sizes in the
+library.  Everything runs on ``stream`` (default: the current one), which has to be a stream of the tensors' device, and
+that device the current one.
+
+    cache = kvc.alloc_cache(batch, n_kv_heads, head_dim, capacity, device=dev)      # one layer
+    kvc.kvc_cache_gather(desc, k, v, idx, n_keep, caches)                            # kept rows, all layers
+    kvc.kvc_rotary(rope, q, k_new, positions, q, k_new)                              # one step of one layer
+    kvc.kvc_cache_append(cache, k_new, v_new, weight=weight)
+    kvc.kvc_attend(cache, q, out, weight=weight, workspace=ws)
+    kvc.kvc_evict(cache, spare, weight, budget, recent, idx, weight_out=spare_weight)    # now and then
+"""
+from __future__ import annotations
+
+import ctypes as C
+import dataclasses
+from typing import Optional, Sequence
+
+import torch
+
+from .binding import (BF16, F32, KvcAttendDesc, KvcCache, KvcError, KvcRopeDesc, _check, _dptr, _load, _ptr_array, _stream, _ws)
+
+INT8, E4M3 = 0, 1
+_SCALING = {"none": 0, "linear": 1, "banded": 2, "yarn": 3}
+_FORMATS = {torch.int8: INT8, torch.float8_e4m3fn: E4M3}
+_DTYPES = {torch.float32: F32, torch.bfloat16: BF16}
+
+
+def _refuse(cond: bool, message: str, *args) -> None:
+    if cond:
+        raise KvcError(-1, message % args if args else message)
+
+
+def _dtype(t: torch.Tensor, name: str) -> int:
+    code = _DTYPES.get(t.dtype)
+    if code is None:
+        raise KvcError(-1, "%s must be bf16 or fp32, not %s" % (name, t.dtype))
+    return code
+
+
+def _rows4(t: torch.Tensor, name: str, batch: int, heads: Optional[int], rows: Optional[int], d: int, dtype=None) -> None:
+    """[batch, heads, rows, d] with contiguous rows."""
+    ok = (t.dim() == 4 and t.shape[0] == batch and t.shape[3] == d and (heads is None or t.shape[1] == heads)
+          and (rows is None or t.shape[2] == rows))
+    _refuse(not ok, "%s has shape %s, not [%s, %s, %s, %s]", name, tuple(t.shape), batch, heads or "heads", rows or "rows", d)
+    _refuse(t.stride(3) != 1, "%s: a row's entries must be contiguous", name)
+    _refuse(dtype is not None and t.dtype != dtype, "%s must be %s, not %s", name, dtype, t.dtype)
+
+
+def _dense(t: Optional[torch.Tensor], name: str, dtype, *shape) -> None:
+    if t is None:
+        return
+    _refuse(t.dtype != dtype, "%s must be %s, not %s", name, dtype, t.dtype)
+    _refuse(tuple(t.shape) != shape, "%s has shape %s, not %s", name, tuple(t.shape), shape)
+    _refuse(not t.is_contiguous(), "%s must be contiguous", name)
+
+
+def _one_device(first: torch.Tensor, *others: Optional[torch.Tensor]) -> None:
+    """All tensors on one device, and that the current one (a launch goes to the current device)."""
+    dev = first.get_device()
+    for t in others:
+        if t is not None and t.get_device() != dev:
+            raise KvcError(-1, "tensors on different devices: %s and %s" % (first.device, t.device))
+    if dev >= 0 and dev != torch.cuda.current_device():
+        raise KvcError(-1, "tensors on %s, which is not the current device" % (first.device,))
+
+
+def _strides(t: torch.Tensor):
+    # (a dimension of one row may have any stride; slot 0 at 0 would mean dense, so a stride for a batch of one is made up)
+    d = t.shape[3]
+    s = [t.stride(i) if t.shape[i] > 1 else 0 for i in range(3)]
+    if s[2] == 0 and t.shape[2] == 1:
+        s[2] = d
+    if s[0] == 0:
+        _refuse(t.shape[0] > 1, "a batch of one row repeated (stride 0) is not supported")
+        s[0] = max(s[1] * t.shape[1], s[2] * t.shape[2])
+    return (C.c_int64 * 3)(*s)
+
+
+class Cache:
+    """An 8-bit cache of one layer (or of layers laid out as one batch) over tensors that the caller keeps.
+
+    k, v      [batch, n_kv_heads, capacity, head_dim], ``torch.int8`` or ``torch.float8_e4m3fn``; a token's entries contiguous
+    k_exp, v_exp   [batch, n_kv_heads, ceil(capacity / block)] int8; lengths [batch, n_kv_heads] int32; contiguous
+    """
+
+    def __init__(self, k: torch.Tensor, v: torch.Tensor, k_exp: torch.Tensor, v_exp: torch.Tensor, lengths: torch.Tensor, block: int):
+        _refuse(k.dim() != 4, "k has %d dimensions, not 4", k.dim())
+        fmt = _FORMATS.get(k.dtype)
+        _refuse(fmt is None, "k must be int8 or float8_e4m3fn, not %s", k.dtype)
+        _refuse(block not in (16, 32, 64, 128), "block must be 16, 32, 64 or 128")
+        b, h, cap, d = k.shape
+        _rows4(k, "k", b, h, cap, d)
+        _rows4(v, "v", b, h, cap, d, k.dtype)
+        blocks = -(-cap // block)
+        _dense(k_exp, "k_exp", torch.int8, b, h, blocks)
+        _dense(v_exp, "v_exp", torch.int8, b, h, blocks)
+        _dense(lengths, "lengths", torch.int32, b, h)
+        dev = k.get_device()
+        for t in (v, k_exp, v_exp, lengths):
+            _refuse(t.get_device() != dev, "the cache's tensors are on different devices")
+        ks = _strides(k)
+        _refuse(list(ks) != list(_strides(v)), "k and v have different strides")
+        self.k, self.v, self.k_exp, self.v_exp, self.lengths, self.block = k, v, k_exp, v_exp, lengths, block
+        self.batch, self.n_kv_heads, self.capacity, self.head_dim, self.format = b, h, cap, d, fmt
+        self.struct = KvcCache(b, h, d, block, fmt, 0, cap, ks, k.data_ptr(), v.data_ptr(), k_exp.data_ptr(), v_exp.data_ptr(),
+                               lengths.data_ptr())
+
+    @property
+    def bytes(self) -> int:
+        return 2 * (self.k.numel() + self.k_exp.numel())
+
+
+def alloc_cache(batch: int, n_kv_heads: int, head_dim: int, capacity: int, block: int = 64, dtype=torch.float8_e4m3fn, device="cuda") -> Cache:
+    """An empty cache."""
+    codes = lambda: torch.zeros((batch, n_kv_heads, capacity, head_dim), dtype=dtype, device=device)  # noqa: E731
+    exps = lambda: torch.zeros((batch, n_kv_heads, -(-capacity // block)), dtype=torch.int8, device=device)  # noqa: E731
+    return Cache(codes(), codes(), exps(), exps(), torch.zeros((batch, n_kv_heads), dtype=torch.int32, device=device), block)
+
+
+@dataclasses.dataclass(frozen=True)
+class Rotary:
+    """Rotary positions of ``rot_dim`` of a head's entries; see ``kvc_rope_desc`` for the scalings."""
+    rot_dim: int
+    theta: float = 10000.0
+    interleaved: bool = False
+    scaling: str = "none"            # "none" | "linear" | "banded" | "yarn"
+    factor: float = 1.0
+    turns_low: float = 1.0
+    turns_high: float = 4.0
+    original_ctx: float = 8192.0
+    mscale: float = 0.0              # 0: the scaling's own
+
+
+def kvc_rotary(rope: Rotary, q: Optional[torch.Tensor], k: Optional[torch.Tensor], positions: torch.Tensor,
+               q_out: Optional[torch.Tensor] = None, k_out: Optional[torch.Tensor] = None, inverse: bool = False, stream=None) -> None:
+    """Turn q [batch, n_q_heads, rows, head_dim] and k [batch, n_kv_heads, rows, head_dim] (either may be None) by
+    ``positions`` ([rows] or [batch, rows], int64).  Outputs default to their inputs (in place)."""
+    x = q if q is not None else k
+    _refuse(x is None, "q and k are both None")
+    _refuse(x.dim() != 4, "q and k have four dimensions")
+    _refuse(rope.scaling not in _SCALING, "unknown scaling %r", rope.scaling)
+    b, _, rows, d = x.shape
+    code = _dtype(x, "q or k")
+    _refuse(q is None and q_out is not None or k is None and k_out is not None, "an output without its input")
+    q_out = q if q_out is None else q_out
+    k_out = k if k_out is None else k_out
+    for t, o, name in ((q, q_out, "q"), (k, k_out, "k")):
+        if t is not None:
+            _rows4(t, name, b, None, rows, d, x.dtype)
+            _rows4(o, name + "_out", b, t.shape[1], rows, d, x.dtype)
+    _refuse(positions.dtype != torch.int64, "positions must be int64, not %s", positions.dtype)
+    _refuse(tuple(positions.shape) not in ((rows,), (b, rows), (1, rows)), "positions has shape %s, not [%d] or [%d, %d]",
+            tuple(positions.shape), rows, b, rows)
+    _refuse(rows > 1 and positions.stride(-1) != 1, "a sequence's positions must be contiguous")
+    _one_device(x, k, positions, q_out, k_out)
+    desc = KvcRopeDesc(b, q.shape[1] if q is not None else 0, k.shape[1] if k is not None else 0, d, rows, rope.rot_dim, code,
+                       int(rope.interleaved), int(inverse), _SCALING[rope.scaling], rope.theta, rope.factor, rope.turns_low,
+                       rope.turns_high, rope.original_ctx, rope.mscale)
+    if q is not None:
+        desc.q_stride, desc.q_out_stride = _strides(q), _strides(q_out)
+    if k is not None:
+        desc.k_stride, desc.k_out_stride = _strides(k), _strides(k_out)
+    per_sequence = positions.stride(0) if positions.dim() == 2 and positions.shape[0] > 1 else 0
+    _check(_load().kvc_rotary(C.byref(desc), _dptr(q), _dptr(k), _dptr(positions), per_sequence, _dptr(q_out), _dptr(k_out),
+                              _stream(stream)))
+
+
+def kvc_cache_gather(desc, k: Sequence[torch.Tensor], v: Sequence[torch.Tensor], idx: Optional[torch.Tensor],
+                     n_keep: Optional[torch.Tensor], caches: Sequence[Cache], per_head: bool = False,
+                     device_status: Optional[torch.Tensor] = None, stream=None) -> None:
+    """``kvc_gather`` into 8-bit caches, one per layer.  idx [L, batch, Hkv, N] int32 or None; n_keep [batch, L] (or, with
+    ``per_head``, [batch, L, Hkv]) int32 or None.  device_status: int32, becomes KVC_ERR_CAPACITY if rows did not fit."""
+    L, b, h, n = desc.n_layers, desc.batch, desc.n_kv_heads, desc.n_ctx
+    _refuse(not (len(k) == len(v) == len(caches) == L), "k, v and caches hold one entry per layer (%d)", L)
+    dtype = torch.float32 if desc.dtype == F32 else torch.bfloat16
+    for t in (*k, *v):
+        _rows4(t, "k or v", b, h, n, desc.head_dim, dtype)
+    given = list(desc.kv_stride) if desc.kv_stride[0] else [h * n * desc.head_dim, n * desc.head_dim, desc.head_dim]
+    for t in (*k, *v):
+        _refuse(any(t.shape[i] > 1 and t.stride(i) != given[i] for i in range(3)), "k or v has other strides than desc.kv_stride")
+    _dense(idx, "idx", torch.int32, L, b, h, n)
+    _dense(n_keep, "n_keep", torch.int32, *((b, L, h) if per_head else (b, L)))
+    _refuse(device_status is not None and device_status.dtype != torch.int32, "device_status must be int32")
+    _one_device(k[0], *k, *v, idx, n_keep, device_status, *(c.k for c in caches))
+    structs = (KvcCache * L)(*(c.struct for c in caches))
+    _check(_load().kvc_cache_gather(C.byref(desc), _ptr_array(k), _ptr_array(v), _dptr(idx), _dptr(n_keep), int(per_head), structs,
+                                    _dptr(device_status), _stream(stream)))
+
+
+def kvc_cache_append(cache: Cache, k_new: torch.Tensor, v_new: torch.Tensor, n_new: Optional[torch.Tensor] = None,
+                     lengths_out: Optional[torch.Tensor] = None, weight: Optional[torch.Tensor] = None,
+                     device_status: Optional[torch.Tensor] = None, stream=None) -> None:
+    """Rows of new tokens [batch, Hkv, rows, head_dim] behind the ones in use; ``n_new`` [batch] int32 of them per sequence."""
+    b, h = cache.batch, cache.n_kv_heads
+    code = _dtype(k_new, "k_new")
+    _rows4(k_new, "k_new", b, h, None, cache.head_dim)
+    _rows4(v_new, "v_new", b, h, k_new.shape[2], cache.head_dim, k_new.dtype)
+    strides = _strides(k_new)
+    _refuse(list(strides) != list(_strides(v_new)), "k_new and v_new have different strides")
+    _dense(n_new, "n_new", torch.int32, b)
+    _dense(lengths_out, "lengths_out", torch.int32, b, h)
+    _dense(weight, "weight", torch.float32, b, h, cache.capacity)
+    _refuse(device_status is not None and device_status.dtype != torch.int32, "device_status must be int32")
+    _one_device(cache.k, k_new, v_new, n_new, lengths_out, weight, device_status)
+    _check(_load().kvc_cache_append(C.byref(cache.struct), _dptr(k_new), _dptr(v_new), code, k_new.shape[2], strides, _dptr(n_new),
+                                    _dptr(lengths_out), _dptr(weight), _dptr(device_status), _stream(stream)))
+
+
+def kvc_cache_read(cache: Cache, k_out: Optional[torch.Tensor], v_out: Optional[torch.Tensor], first: Optional[torch.Tensor] = None,
+                   stream=None) -> None:
+    """Values of the rows first[b, h] .. into k_out, v_out [batch, Hkv, rows, head_dim] (bf16 or fp32, contiguous)."""
+    x = k_out if k_out is not None else v_out
+    _refuse(x is None, "k_out and v_out are both None")
+    code = _dtype(x, "k_out or v_out")
+    _refuse(x.dim() != 4, "k_out and v_out have four dimensions")
+    for t in (k_out, v_out):
+        _dense(t, "k_out or v_out", x.dtype, cache.batch, cache.n_kv_heads, x.shape[2], cache.head_dim)
+    _dense(first, "first", torch.int32, cache.batch, cache.n_kv_heads)
+    _one_device(cache.k, k_out, v_out, first)
+    _check(_load().kvc_cache_read(C.byref(cache.struct), _dptr(first), x.shape[2], code, _dptr(k_out), _dptr(v_out), _stream(stream)))
+
+
+def _attend_desc(cache: Cache, q: torch.Tensor, out: Optional[torch.Tensor], causal: bool, scale: float) -> KvcAttendDesc:
+    code = _dtype(q, "q")
+    _rows4(q, "q", cache.batch, None, None, cache.head_dim)
+    desc = KvcAttendDesc(q.shape[1], q.shape[2], code, int(causal), scale, 0, _strides(q))
+    if out is not None:
+        _rows4(out, "out", cache.batch, q.shape[1], q.shape[2], cache.head_dim, q.dtype)
+        desc.out_stride = _strides(out)
+    return desc
+
+
+def kvc_attend_workspace_size(cache: Cache, q: torch.Tensor, with_weight: bool) -> int:
+    """Bytes of scratch ``kvc_attend`` needs for queries of q's shape; with_weight: with the tokens' weights."""
+    out = C.c_size_t(0)
+    desc = _attend_desc(cache, q, None, True, 0.0)
+    _check(_load().kvc_attend_workspace_size(C.byref(cache.struct), C.byref(desc), int(with_weight), C.byref(out)))
+    return int(out.value)
+
+
+def kvc_attend(cache: Cache, q: torch.Tensor, out: torch.Tensor, lse: Optional[torch.Tensor] = None,
+               weight: Optional[torch.Tensor] = None, weight_out: Optional[torch.Tensor] = None,
+               row_counts: Optional[torch.Tensor] = None, causal: bool = True, scale: float = 0.0,
+               workspace: Optional[torch.Tensor] = None, stream=None) -> None:
+    """Attention of q [batch, n_q_heads, rows, head_dim] over the cache into out.  lse [batch, n_q_heads, rows] fp32.
+    weight [batch, Hkv, capacity] fp32: the tokens' running weight, added to in place, or into ``weight_out``."""
+    desc = _attend_desc(cache, q, out, causal, scale)
+    b, h = cache.batch, cache.n_kv_heads
+    if weight_out is None:
+        weight_out = weight
+    _dense(lse, "lse", torch.float32, b, q.shape[1], q.shape[2])
+    _dense(weight, "weight", torch.float32, b, h, cache.capacity)
+    _dense(weight_out, "weight_out", torch.float32, b, h, cache.capacity)
+    _dense(row_counts, "row_counts", torch.int32, b)
+    _one_device(cache.k, q, out, lse, weight, weight_out, row_counts, workspace)
+    wp, wb = _ws(workspace)
+    _check(_load().kvc_attend(C.byref(cache.struct), C.byref(desc), _dptr(q), _dptr(row_counts), _dptr(out), _dptr(lse), _dptr(weight),
+                              _dptr(weight_out), wp, wb, _stream(stream)))
+
+
+def kvc_evict(src: Cache, dst: Cache, weight: torch.Tensor, budget: int, recent: int, idx_out: torch.Tensor,
+              weight_out: Optional[torch.Tensor] = None, stream=None) -> None:
+    """The last ``recent`` rows of every head and the heaviest of the others, ``budget`` in all, from src into dst; their
+    positions go to idx_out [batch, Hkv, budget] int32, their weights to weight_out [batch, Hkv, dst.capacity]."""
+    b, h = src.batch, src.n_kv_heads
+    _dense(weight, "weight", torch.float32, b, h, src.capacity)
+    _dense(idx_out, "idx_out", torch.int32, b, h, int(budget))
+    _dense(weight_out, "weight_out", torch.float32, b, h, dst.capacity)
+    _one_device(src.k, dst.k, weight, idx_out, weight_out)
+    _check(_load().kvc_evict(C.byref(src.struct), C.byref(dst.struct), _dptr(weight), int(budget), int(recent), _dptr(idx_out),
+                             _dptr(weight_out), _stream(stream)))
