@@ -107,9 +107,11 @@ def cache_values(cache):
     return out
 
 
-def attend(q, k, v, lengths, causal, scale, counts=None):
+def attend(q, k, v, lengths, causal, scale, counts=None, step=None, small=0.0):
     """q [b, hq, rows, d], k, v [b, h, n, d], all in 64 bits.  Returns out, lse, the weight each token gets, sum p |v| (what
-    errors of p are measured against) and the largest sum |q k| scale (what errors of a logit are)."""
+    errors of p are measured against) and the largest sum |q k| scale (what errors of a logit are).  step [b, h, n]: what one
+    unit of a V code stands for; sum p |v| then gets a term for P's smallest steps, `small` of the row's largest p times step
+    for each token and codes of up to 448."""
     b, hq, rows, d = q.shape
     h, n = k.shape[1], k.shape[2]
     out, lse = torch.zeros_like(q), torch.full((b, hq, rows), -math.inf, dtype=torch.float64)
@@ -128,6 +130,8 @@ def attend(q, k, v, lengths, causal, scale, counts=None):
                 size = max(size, float((kk.abs() @ q[i, j, r].abs()).max() * scale))
                 p = torch.softmax(s, 0)
                 out[i, j, r], mass[i, j, r] = p @ vv, p @ vv.abs()
+                if step is not None:
+                    mass[i, j, r] += seen * small * 448.0 * float((p * step[i, g, :seen]).max())
                 lse[i, j, r] = torch.logsumexp(s, 0)
                 weight[i, g, :seen] += p
     return out, lse, weight, mass, size

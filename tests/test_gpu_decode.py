@@ -292,14 +292,18 @@ def _check_attend(c, q, out, lse, weight, weight0, causal, scale, counts=None):
     rounded to 11 bits in front of V and the sum to bf16; fp32: p to 22 bits and the sums of up to thousands of terms, kept in
     fp32 by parts, within 2^-19."""
     k, v = _clean_values(c)
-    o, l, w, mass, size = R.attend(q.cpu().double(), k, v, c.lengths.cpu(), causal, scale, counts)
+    # P 2^15 in fp16 (or, for fp32, what is left of it after the first fp16), relative to the row's largest p 2^e: numbers below
+    # 2^-14 have steps of 2^-24, so p 2^e is off by up to half of 2^-39 of that largest one, for codes of up to 448
+    step = torch.pow(torch.tensor(2.0, dtype=torch.float64), c.v_exp.cpu().double()).repeat_interleave(c.block, -1)[..., :c.capacity]
+    rel = 2.0 ** -11 if q.dtype == BF else 2.0 ** -19
+    o, l, w, mass, size = R.attend(q.cpu().double(), k, v, c.lengths.cpu(), causal, scale, counts, step, 2.0 ** -39 / rel)
     dp = 2 * (2.0 ** -19 * size + 2.0 ** -19)
     bf = q.dtype == BF
     got = out.cpu().double()
     rows = torch.ones_like(o, dtype=torch.bool)
     if counts is not None:
         rows = (torch.arange(q.shape[2]) < counts[:, None])[:, None, :, None].expand_as(o)
-    tol = (dp + (2.0 ** -11 if bf else 2.0 ** -19)) * mass + (2.0 ** -8 if bf else 2.0 ** -23) * o.abs() + 1e-30
+    tol = (dp + rel) * mass + (2.0 ** -8 if bf else 2.0 ** -23) * o.abs() + 1e-30
     err = ((got - o).abs() - tol)[rows]
     assert torch.isfinite(got[rows]).all() and (err <= 0).all(), float(err.max())
     if lse is not None:
