@@ -2,16 +2,17 @@
 //
 // HBM is the bound: 2 d bytes of codes per token and KV head, against 4 d products per query row.  Two kernels:
 //
-// attend_split_kernel   one CTA per SM.  The tokens of all heads, in granules of kGranule, are laid end to end and cut into
-//   equal shares, one per CTA, whatever the lengths: a CTA may hold a part of one long head or many short ones.  Its warps
-//   take 32 tokens in turn, each for itself: a lane copies the very 16-byte pieces it will use (cp.async into its own
-//   places in shared memory, kStages deep, no barrier), turns the codes into fp16 and feeds mma.m16n8k16: S^T = K Q^T with the
-//   tokens as rows, then O^T = V^T P^T, eight query rows to a column tile (kTiles of them share the converted codes).
-//   Operand layouts: the order of the summed index is free as long as both operands agree, so lane (g, t) takes token
-//   g's entries 16 t .. 16 t + 15 of each 64 as its k slots, and entries (d / 8) g .. of its tokens of V as its rows; a
-//   transpose of P's 8 x 8 tiles (movmatrix) is the only exchange between lanes.  Legacy mma on purpose: the tensor pipe needs
-//   a quarter of the time the codes take to arrive, and codes go from registers into it; through tcgen05 they would have to
-//   be written back to shared memory as fp16 first.
+// attend_split_kernel   one CTA per SM.  The tokens of all heads, in granules of kGranule (and kSetup granules more per head,
+//   for what starting one costs), are laid end to end and cut into equal shares, one per CTA, whatever the lengths.  A CTA
+//   whose share lies within one head spreads it over its warps, 32 tokens each in turn, and joins their results; one that
+//   holds several heads cuts its share once more, one piece per warp, and each warp works for itself.  A lane copies the very
+//   16-byte pieces it will use (cp.async into its own places in shared memory, kStages deep, no barrier), turns the codes into
+//   fp16 and feeds mma.m16n8k16: S^T = K Q^T with the tokens as rows, then O^T = V^T P^T, eight query rows to a column tile
+//   (kTiles of them share the converted codes).  Operand layouts: the order of the summed index is free as long as both
+//   operands agree, so lane (g, t) takes token g's entries 16 t .. 16 t + 15 of each 64 as its k slots, and entries (d / 8) g ..
+//   of its tokens of V as its rows; a transpose of P's 8 x 8 tiles (movmatrix) is the only exchange between lanes.  Legacy
+//   mma on purpose: an SM scheduler has 44 clocks per token before the codes arrive from HBM and mma takes 8 of them (8.0 clk
+//   per m16n8k16, measured); through tcgen05 the converted codes would have to go back to shared memory first.
 // attend_join_kernel    joins the parts of a row (log-sum-exp), and adds the row's weights from the logits, which the first
 //   kernel leaves in the workspace (they stay in L2; the softmax's denominator is known only after the last token).
 //
@@ -28,9 +29,9 @@
 namespace kvc {
 namespace {
 
-constexpr int kWarps = 12;                // (8: xx, 16 do not fit the registers)
-constexpr int kAttThreads = kWarps * 32;
 constexpr int kGranule = 64;              // tokens: unit of the split
+constexpr int kSetup = 2;                 // granules that a head's start counts as
+constexpr int kMaxWarps = 12;
 constexpr int kMaxCtas = 256;             // bounds the workspace, whatever the device
 constexpr int kMaxRows = 64;              // query rows of a KV head that one launch takes (bounds the logits kept)
 constexpr float kLift = 15.f;             // P goes into V as 2^15 p: fp16 then tells weights apart down to 2^-40 of the largest
@@ -44,10 +45,11 @@ struct AttendParams {
   float scale;
   long long qs[3], os[3];
   // of this launch: query rows row0 .. row0 + live - 1 of the G * rows of a KV head, in row_tiles tiles of 8 * kTiles
-  int row0, live, row_tiles, tile_rows, ctas, logit_rows;
+  int row0, live, row_tiles, tile_rows, ctas, warps, logit_rows;
   float* part_o;                          // [slot][tile_rows][d]
   float2* part_ml;                        // [slot][tile_rows]: largest logit (in powers of two), sum of 2^(logit - it)
   float* logits;                          // [unit][row tile][token][logit_rows]
+  long long* before;                      // [units + 1]: granules (with kSetup) in front of a head, per row tile; all of them last
 };
 
 __device__ __forceinline__ float ex2(float x) {
@@ -56,7 +58,7 @@ __device__ __forceinline__ float ex2(float x) {
   return y;
 }
 __device__ __forceinline__ void mma16816(float* c, const uint32_t* a, uint32_t b0, uint32_t b1) {
-  asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+  asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
                : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
                : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
@@ -108,127 +110,223 @@ __device__ __forceinline__ long long tokens_seen(const AttendParams& P, int rr, 
   const long long n = P.causal ? len - (rows - 1 - m) : len;
   return n < 0 ? 0 : n;
 }
-// CTAs that get a share of `total` granules: each at least one, so that the parts of a head lie in consecutive CTAs.
-__device__ __forceinline__ int sharers(const AttendParams& P, long long total) { return total < P.ctas ? max((int)total, 1) : P.ctas; }
-__device__ __forceinline__ int granules(const AttendParams& P, int unit) { return (int)((P.c.length(unit) + kGranule - 1) / kGranule); }
+// Granules of a head's row tile, what starting it costs included.
+__device__ __forceinline__ int granules(long long len) { return len == 0 ? 0 : (int)((len + kGranule - 1) / kGranule) + kSetup; }
 
-template <int kFormat, int kD, int kTiles, bool kSplitF32, bool kWeight>
-struct Warp {
+// a / b of non-negative numbers; nearly always 32-bit ones, whose division takes a fraction of the time.
+__device__ __forceinline__ long long quotient(long long a, long long b) {
+  return ((a | b) >> 32) == 0 ? (long long)((uint32_t)a / (uint32_t)b) : a / b;
+}
+
+// `total` granules cut into `parts` shares, as many of them as there are granules at most: share i, and the share of a place.
+// The first `more` shares hold one granule more than the others.
+struct Shares {
+  long long each;
+  int parts, more;
+  __device__ __forceinline__ Shares(long long total, int parts_) : parts(total < parts_ ? (int)total : parts_) {
+    each = quotient(total, parts);
+    more = (int)(total - each * parts);
+  }
+  __device__ __forceinline__ long long begin(int i) const { return each * i + min(i, more); }
+  __device__ __forceinline__ int of(long long place) const {
+    const long long larger = more * (each + 1);
+    return place < larger ? (int)quotient(place, each + 1) : more + (int)quotient(place - larger, each);
+  }
+};
+
+// Warps, stages and shared memory of a form of attend_split_kernel.
+template <typename T, int kD, int kTiles>
+struct Form {
+  static constexpr bool kTwo = sizeof(T) == 4;         // fp32: Q and P as two fp16 each
+  static constexpr bool kQShared = kTiles == 4;        // Q's operands in shared memory (else in registers)
+  static constexpr int kWarps = kTiles == 1 ? 12 : kTiles == 2 && !kTwo ? 10 : 8;
+  static constexpr int kThreads = kWarps * 32;
   static constexpr int kSteps = kD / 16;               // k steps of Q K^T, and row tiles of V^T
   static constexpr int kKPieces = kD / 64;             // 16-byte pieces of a token's K per lane
   static constexpr int kVBytes = kD / 8;               // a lane's bytes of a token's V
   static constexpr int kStages = kD == 128 ? 2 : 3;
   static constexpr int kStageBytes = 32 * 2 * kD;      // per warp: 32 tokens of K and V
   static constexpr int kVBase = 32 * kD;
+  static constexpr int kRows = 8 * kTiles;
+  static constexpr int kPitch = kD + 4;
+  static constexpr int kQBytes = kQShared ? kTiles * kSteps * 32 * 8 : 0;      // per warp
+  static constexpr int kWarpBytes = kStages * kStageBytes + kQBytes;
+  static constexpr int kJoinBytes = kWarps * kRows * kPitch * 4;
+  static constexpr int kSmem = kWarps * kWarpBytes > kJoinBytes ? kWarps * kWarpBytes : kJoinBytes;
 };
 
 template <typename T, int kFormat, int kD, int kTiles, bool kWeight>
-__global__ void __launch_bounds__(kAttThreads, 1)
+__global__ void __launch_bounds__(Form<T, kD, kTiles>::kThreads, 1)
 attend_split_kernel(const __grid_constant__ AttendParams P, const T* __restrict__ q, const int32_t* __restrict__ row_counts) {
-  constexpr bool kTwo = sizeof(T) == 4;                // fp32: Q and P as two fp16 each
-  using W = Warp<kFormat, kD, kTiles, kTwo, kWeight>;
-  constexpr int kSteps = W::kSteps, kStages = W::kStages, kRowsTile = 8 * kTiles, kPitch = kD + 4;
+  using F = Form<T, kD, kTiles>;
+  constexpr bool kTwo = F::kTwo;
+  constexpr int kWarps = F::kWarps, kThreads = F::kThreads, kSteps = F::kSteps, kStages = F::kStages, kRows = F::kRows, kPitch = F::kPitch;
   extern __shared__ __align__(128) char smem[];
   __shared__ long long s_sum[kWarps];
-  __shared__ int s_unit;
-  __shared__ long long s_before, s_total;
-  __shared__ float s_stat[kWarps][kRowsTile][2];
+  __shared__ int s_unit[kWarps + 1];                   // the head that each warp's piece starts in; last: the whole share's
+  __shared__ long long s_before[kWarps + 1];
+  __shared__ float s_stat[kWarps][kRows][2];
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t = lane & 3;
   grid_dependency_wait();
+  asm volatile("griddepcontrol.launch_dependents;");   // (attend_join_kernel may come up; it waits for this grid's end itself)
   const Cache& c = P.c;
   const int units = c.units();
 
-  // ---- this CTA's share: granules [at, end) of all of them, and the unit that `at` lies in
-  {
-    const int per = (units + kAttThreads - 1) / kAttThreads;
-    const int u0 = tid * per, u1 = min(u0 + per, units);
-    long long mine = 0;
-    for (int u = u0; u < u1; ++u) mine += granules(P, u);
-    long long incl = mine;
+  // ---- this CTA's share, and the heads that it and its warps' pieces start in
+  const int per = (units + kThreads - 1) / kThreads;
+  const int u0 = tid * per, u1 = min(u0 + per, units);
+  long long mine = 0;
+  for (int u = u0; u < u1; ++u) mine += granules(c.length(u));
+  long long incl = mine;
 #pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-      const long long y = __shfl_up_sync(0xffffffffu, incl, o);
-      if (lane >= o) incl += y;
-    }
-    if (lane == 31) s_sum[warp] = incl;
-    __syncthreads();
-    long long total = 0;
-    for (int w = 0; w < kWarps; ++w) {
-      if (w < warp) incl += s_sum[w];
-      total += s_sum[w];
-    }
-    total *= P.row_tiles;
-    const long long at = total * blockIdx.x / sharers(P, total);
-    long long before = (incl - mine) * P.row_tiles;
-    if (tid == 0) s_total = total;
-    if (total > 0 && before <= at && at < incl * P.row_tiles) {
-      int u = u0;
-      for (;; ++u) {
-        const long long n = (long long)granules(P, u) * P.row_tiles;
-        if (at < before + n) break;
-        before += n;
-      }
-      s_unit = u;
-      s_before = before;
-    }
-    __syncthreads();
+  for (int o = 1; o < 32; o <<= 1) {
+    const long long y = __shfl_up_sync(0xffffffffu, incl, o);
+    if (lane >= o) incl += y;
   }
-  const long long total = s_total;
-  const int ctas = sharers(P, total);
-  if (total == 0 || (int)blockIdx.x >= ctas) return;
-  long long at = total * blockIdx.x / ctas;
-  const long long end = total * (blockIdx.x + 1) / ctas;
-  int unit = s_unit;
-  long long before = s_before;
+  if (lane == 31) s_sum[warp] = incl;
+  __syncthreads();
+  long long total = 0;
+#pragma unroll
+  for (int w = 0; w < kWarps; ++w) {
+    if (w < warp) incl += s_sum[w];
+    total += s_sum[w];
+  }
+  if (blockIdx.x == 0) {                               // for attend_join_kernel
+    long long b = incl - mine;
+    for (int u = u0; u < u1; ++u) {
+      P.before[u] = b;
+      b += granules(c.length(u));
+    }
+    if (tid == 0) P.before[units] = total;
+  }
+  total *= P.row_tiles;
+  if (total == 0) return;
+  const Shares ctas(total, P.ctas);
+  if ((int)blockIdx.x >= ctas.parts) return;
+  const long long share0 = ctas.begin(blockIdx.x), share1 = ctas.begin(blockIdx.x + 1);
+  const Shares pieces(share1 - share0, kWarps);
+  if (mine > 0) {
+    long long v = (incl - mine) * P.row_tiles;
+    if (v < share1 && incl * P.row_tiles > share0) {
+      for (int u = u0; u < u1; ++u) {
+        const long long n = (long long)granules(c.length(u)) * P.row_tiles;
+        if (v <= share0 && share0 < v + n) { s_unit[kWarps] = u; s_before[kWarps] = v; }
+        for (int w = 0; w < pieces.parts; ++w) {
+          const long long p = share0 + pieces.begin(w);
+          if (v <= p && p < v + n) { s_unit[w] = u; s_before[w] = v; }
+        }
+        v += n;
+      }
+    }
+  }
+  __syncthreads();
+  // within one row tile of one head: all warps work on it together
+  bool together;
+  long long at, end, before;                           // the place, its end, where the row tile begins
+  int unit, n_gran, rt;
+  long long len;
+  {
+    unit = s_unit[kWarps];
+    before = s_before[kWarps];
+    n_gran = granules(c.length(unit));
+    if (P.row_tiles > 1) before += quotient(share0 - before, n_gran) * n_gran;
+    together = share1 <= before + n_gran;
+    at = share0;
+    end = share1;
+    if (!together) {
+      if (warp >= pieces.parts) return;                // (no barrier follows for a CTA of several heads)
+      at = share0 + pieces.begin(warp);
+      end = share0 + pieces.begin(warp + 1);
+      unit = s_unit[warp];
+      before = s_before[warp];
+    }
+    len = c.length(unit);
+    n_gran = granules(len);
+    rt = P.row_tiles > 1 ? (int)quotient(at - (together ? s_before[kWarps] : before), n_gran) : 0;
+    before = (together ? s_before[kWarps] : before) + (long long)rt * n_gran;
+  }
+  const int warp_in = together ? warp : 0, warps_in = together ? kWarps : 1;
+  const int st = (int)c.st[2];                         // (a row's stride; 31 bits, checked by the host)
 
-  char* my_smem = smem + warp * (kStages * W::kStageBytes);
+  char* my_smem = smem + warp * F::kWarpBytes;
   const uint32_t my_smem_addr = (uint32_t)__cvta_generic_to_shared(my_smem);
-  int rt = (int)((at - before) / granules(P, unit));
-  before += (long long)rt * granules(P, unit);
 
   while (true) {
     // ---- a part of one row tile of one head: tokens [lo, hi)
     const int b = unit / c.Hkv, h = unit - b * c.Hkv;
-    const long long len = c.length(unit);
-    const int n_gran = granules(P, unit);
-    const long long lo = (at - before) * kGranule;
-    const long long upto = min(end - before, (long long)n_gran);
-    const long long hi = min(upto * kGranule, len);
+    const long long upto = min(end, before + n_gran);
+    const int lo = max((int)(at - before) - kSetup, 0) * kGranule;
+    const int hi = min((long long)max((int)(upto - before) - kSetup, 0) * kGranule, len);
     const int rows = row_count(P, row_counts, b);
-    const int first_row = P.row0 + rt * kRowsTile, last_row = min(P.row0 + P.live, first_row + kRowsTile);
+    const int first_row = P.row0 + rt * kRows, last_row = min(P.row0 + P.live, first_row + kRows);
+    const int live_rows = last_row - first_row;
 
-    const uint8_t *kc = c.k + c.base(unit), *vc = c.v + c.base(unit);
+    if (hi > lo) {
     const int8_t *ke = c.k_exp + (long long)unit * c.blocks, *ve = c.v_exp + (long long)unit * c.blocks;
-    const int iters = (int)((hi - lo + 32 * kWarps - 1 - 32 * warp) / (32 * kWarps));      // 0 for warps behind the end
+    const int stride = 32 * warps_in;                  // tokens from one step of a warp to its next
+    const int first = lo + 32 * warp_in;
+    const int iters = hi > first ? (hi - first + stride - 1) / stride : 0;
+    // the lane's places in the next 32 tokens to copy
+    const uint8_t* kp = c.k + c.base(unit) + (long long)(first + g) * st + 16 * t;
+    const uint8_t* vp = c.v + c.base(unit) + (long long)(first + 2 * t) * st + F::kVBytes * g;
+    const long long advance = (long long)stride * st;
 
-    auto fetch = [&](int it) {                       // 32 tokens of K and V into stage it % kStages
+    auto fetch = [&](int it) {                         // step `it` into stage it % kStages
       if (it < iters) {
-        const uint32_t dst = my_smem_addr + (it % kStages) * W::kStageBytes;
-        const long long tok0 = lo + (long long)(it * kWarps + warp) * 32;
+        const uint32_t dst = my_smem_addr + (it % kStages) * F::kStageBytes;
+        const int left = hi - first - it * stride;     // tokens from this step on
+        if (left >= 32) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const long long tok = tok0 + 8 * i + g;
-          const bool live = tok < hi;
-          const uint8_t* src = kc + (live ? tok : 0) * c.st[2] + 16 * t;
+          for (int i = 0; i < 4; ++i)
 #pragma unroll
-          for (int p = 0; p < W::kKPieces; ++p) copy_async<16>(dst + ((i * W::kKPieces + p) * 32 + lane) * 16, src + 64 * p, live);
+            for (int p = 0; p < F::kKPieces; ++p)
+              copy_async<16>(dst + ((i * F::kKPieces + p) * 32 + lane) * 16, kp + (long long)(8 * i) * st + 64 * p, true);
+#pragma unroll
+          for (int i = 0; i < 8; ++i)
+            copy_async<F::kVBytes>(dst + F::kVBase + (i * 32 + lane) * F::kVBytes,
+                                   vp + (long long)(16 * (i >> 2) + 8 * ((i >> 1) & 1) + (i & 1)) * st, true);
+        } else {                                       // rows behind the end are filled with zeros, their addresses not used
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const bool live = 8 * i + g < left;
+#pragma unroll
+            for (int p = 0; p < F::kKPieces; ++p)
+              copy_async<16>(dst + ((i * F::kKPieces + p) * 32 + lane) * 16, live ? kp + (long long)(8 * i) * st + 64 * p : c.k, live);
+          }
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            const int tok = 16 * (i >> 2) + 8 * ((i >> 1) & 1) + (i & 1);
+            const bool live = tok + 2 * t < left;
+            copy_async<F::kVBytes>(dst + F::kVBase + (i * 32 + lane) * F::kVBytes, live ? vp + (long long)tok * st : c.v, live);
+          }
         }
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          const long long tok = tok0 + 16 * (i >> 2) + 8 * ((i >> 1) & 1) + 2 * t + (i & 1);
-          const bool live = tok < hi;
-          copy_async<W::kVBytes>(dst + W::kVBase + (i * 32 + lane) * W::kVBytes, vc + (live ? tok : 0) * c.st[2] + W::kVBytes * g, live);
-        }
+        kp += advance;
+        vp += advance;
       }
       copy_commit();
     };
 #pragma unroll
     for (int s = 0; s < kStages - 1; ++s) fetch(s);
 
+    // exponents of the two halves of 32 tokens, read one step ahead
+    int ek[2], ev[2], ek_next[2] = {0, 0}, ev_next[2] = {0, 0};
+    auto fetch_exps = [&](int it) {
+#pragma unroll
+      for (int f = 0; f < 2; ++f) {
+        const int tok = first + it * stride + 16 * f;
+        if (it < iters && tok < hi) {
+          ek_next[f] = __ldg(ke + (tok >> c.block_shift));
+          ev_next[f] = __ldg(ve + (tok >> c.block_shift));
+        }
+      }
+    };
+    fetch_exps(0);
+
     // ---- Q: row 8 n + g of the tile, its entries in the lane's k slots, scaled by a power of two to below 2
-    uint32_t qh[kTiles][kSteps][2], ql[kTwo ? kTiles : 1][kTwo ? kSteps : 1][2];
-    float factor[kTiles][2];                         // of the columns 2 t, 2 t + 1: logit = accumulator * factor * 2^ke
-    int seen[kTiles][2], seen_least = 0x7fffffff;    // (lengths fit 31 bits)
+    uint32_t qh[F::kQShared ? 1 : kTiles][kSteps][2], ql[kTwo ? kTiles : 1][kTwo ? kSteps : 1][2];
+    uint2* sq = reinterpret_cast<uint2*>(my_smem + kStages * F::kStageBytes) + lane;      // [tile][step][lane]
+    float factor[kTiles][2];                           // of the columns 2 t, 2 t + 1: logit = accumulator * factor * 2^ke
+    int seen[kTiles][2], seen_least = 0x7fffffff;      // (lengths fit 31 bits)
 #pragma unroll
     for (int n = 0; n < kTiles; ++n) {
       const int rr = first_row + 8 * n + g;
@@ -253,16 +351,24 @@ attend_split_kernel(const __grid_constant__ AttendParams P, const T* __restrict_
       const int e = min(max((int)(__float_as_uint(top) >> 23) - 127, -120), 126);
       const float down = pow2(-e), up = pow2(e) * P.scale * 1.44269504088896341f;
 #pragma unroll
-      for (int s = 0; s < kSteps; ++s)
+      for (int s = 0; s < kSteps; ++s) {
+        uint32_t w[2];
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
           const float a = x[4 * s + 2 * i] * down, z = x[4 * s + 2 * i + 1] * down;
-          qh[n][s][i] = pack_half2(a, z);
+          w[i] = pack_half2(a, z);
           if (kTwo) {
-            const __half2 hh = *reinterpret_cast<const __half2*>(&qh[n][s][i]);
+            const __half2 hh = *reinterpret_cast<const __half2*>(&w[i]);
             ql[n][s][i] = pack_half2(a - __low2float(hh), z - __high2float(hh));
           }
         }
+        if (F::kQShared) {
+          sq[(n * kSteps + s) * 32] = make_uint2(w[0], w[1]);      // (its own lane reads it back)
+        } else {
+          qh[n][s][0] = w[0];
+          qh[n][s][1] = w[1];
+        }
+      }
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
         factor[n][i] = __shfl_sync(0xffffffffu, up, (2 * t + i) * 4);
@@ -285,53 +391,57 @@ attend_split_kernel(const __grid_constant__ AttendParams P, const T* __restrict_
     float* logit_row = nullptr;
     if (kWeight) logit_row = P.logits + ((long long)unit * P.row_tiles + rt) * c.cap * P.logit_rows + 2 * t;
 
-    // exponents of the two halves of 32 tokens, read one step ahead
-    int ek[2], ev[2], ek_next[2] = {0, 0}, ev_next[2] = {0, 0};
-    auto fetch_exps = [&](int it) {
-#pragma unroll
-      for (int f = 0; f < 2; ++f) {
-        const long long tok = lo + (long long)(it * kWarps + warp) * 32 + 16 * f;
-        if (it < iters && tok < hi) {
-          ek_next[f] = __ldg(ke + (tok >> c.block_shift));
-          ev_next[f] = __ldg(ve + (tok >> c.block_shift));
-        }
-      }
-    };
-    fetch_exps(0);
-
     for (int it = 0; it < iters; ++it) {
       ek[0] = ek_next[0]; ek[1] = ek_next[1]; ev[0] = ev_next[0]; ev[1] = ev_next[1];
       fetch_exps(it + 1);
       fetch(it + kStages - 1);
       copy_wait<kStages - 1>();
-      const char* st = my_smem + (it % kStages) * W::kStageBytes;
-      const long long tok0 = lo + (long long)(it * kWarps + warp) * 32;
+      const char* stage = my_smem + (it % kStages) * F::kStageBytes;
+      const int tok0 = first + it * stride;
 
       // ---- logits, in powers of two: lane holds tokens g and g + 8 (of each 16), columns 2 t and 2 t + 1
       float sc[2][kTiles][4];
 #pragma unroll
-      for (int f = 0; f < 2; ++f) {
+      for (int f = 0; f < 2; ++f)
 #pragma unroll
         for (int n = 0; n < kTiles; ++n)
 #pragma unroll
           for (int i = 0; i < 4; ++i) sc[f][n][i] = 0.f;
 #pragma unroll
-        for (int p = 0; p < W::kKPieces; ++p) {
-          const uint4 w0 = *reinterpret_cast<const uint4*>(st + (((2 * f) * W::kKPieces + p) * 32 + lane) * 16);
-          const uint4 w1 = *reinterpret_cast<const uint4*>(st + (((2 * f + 1) * W::kKPieces + p) * 32 + lane) * 16);
-          const uint32_t x0[4] = {w0.x, w0.y, w0.z, w0.w}, x1[4] = {w1.x, w1.y, w1.z, w1.w};
+      for (int p = 0; p < F::kKPieces; ++p) {
+        uint32_t x[4][4];
 #pragma unroll
-          for (int s = 0; s < 4; ++s) {
-            uint32_t a[4];
-            to_half2<kFormat>(x0[s], &a[0], &a[2]);
-            to_half2<kFormat>(x1[s], &a[1], &a[3]);
+        for (int i = 0; i < 4; ++i) {
+          const uint4 w = *reinterpret_cast<const uint4*>(stage + ((i * F::kKPieces + p) * 32 + lane) * 16);
+          x[i][0] = w.x; x[i][1] = w.y; x[i][2] = w.z; x[i][3] = w.w;
+        }
 #pragma unroll
-            for (int n = 0; n < kTiles; ++n) {
-              mma16816(sc[f][n], a, qh[n][4 * p + s][0], qh[n][4 * p + s][1]);
-              if (kTwo) mma16816(sc[f][n], a, ql[n][4 * p + s][0], ql[n][4 * p + s][1]);
+        for (int s = 0; s < 4; ++s) {
+          uint32_t a[2][4];
+#pragma unroll
+          for (int f = 0; f < 2; ++f) {
+            to_half2<kFormat>(x[2 * f][s], &a[f][0], &a[f][2]);
+            to_half2<kFormat>(x[2 * f + 1][s], &a[f][1], &a[f][3]);
+          }
+#pragma unroll
+          for (int n = 0; n < kTiles; ++n) {
+            uint32_t b0, b1;
+            if (F::kQShared) {
+              const uint2 w = sq[(n * kSteps + 4 * p + s) * 32];
+              b0 = w.x; b1 = w.y;
+            } else {
+              b0 = qh[n][4 * p + s][0]; b1 = qh[n][4 * p + s][1];
+            }
+#pragma unroll
+            for (int f = 0; f < 2; ++f) {
+              mma16816(sc[f][n], a[f], b0, b1);
+              if (kTwo) mma16816(sc[f][n], a[f], ql[n][4 * p + s][0], ql[n][4 * p + s][1]);
             }
           }
         }
+      }
+#pragma unroll
+      for (int f = 0; f < 2; ++f) {
         const float kf = pow2_clamped(ek[f]);
 #pragma unroll
         for (int n = 0; n < kTiles; ++n)
@@ -352,12 +462,12 @@ attend_split_kernel(const __grid_constant__ AttendParams P, const T* __restrict_
         for (int f = 0; f < 2; ++f)
 #pragma unroll
           for (int i = 0; i < 2; ++i) {
-            const long long tok = tok0 + 16 * f + 8 * i + g;
+            const int tok = tok0 + 16 * f + 8 * i + g;
             if (tok < hi) {
 #pragma unroll
               for (int n = 0; n < kTiles; ++n)
                 if (8 * n + 2 * t < P.logit_rows)
-                  *reinterpret_cast<float2*>(logit_row + tok * P.logit_rows + 8 * n) = make_float2(sc[f][n][2 * i], sc[f][n][2 * i + 1]);
+                  *reinterpret_cast<float2*>(logit_row + (long long)tok * P.logit_rows + 8 * n) = make_float2(sc[f][n][2 * i], sc[f][n][2 * i + 1]);
             }
           }
       }
@@ -435,20 +545,20 @@ attend_split_kernel(const __grid_constant__ AttendParams P, const T* __restrict_
             }
           }
         }
-        const char* sv = st + W::kVBase + (4 * f * 32 + lane) * W::kVBytes;
-        uint32_t v[4][W::kVBytes / 4];
+        const char* sv = stage + F::kVBase + (4 * f * 32 + lane) * F::kVBytes;
+        uint32_t v[4][F::kVBytes / 4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           if (kD == 128) {
-            const uint4 w = *reinterpret_cast<const uint4*>(sv + i * 32 * W::kVBytes);
-            v[i][0] = w.x; v[i][1] = w.y; v[i][W::kVBytes / 4 - 2] = w.z; v[i][W::kVBytes / 4 - 1] = w.w;
+            const uint4 w = *reinterpret_cast<const uint4*>(sv + i * 32 * F::kVBytes);
+            v[i][0] = w.x; v[i][1] = w.y; v[i][F::kVBytes / 4 - 2] = w.z; v[i][F::kVBytes / 4 - 1] = w.w;
           } else {
-            const uint2 w = *reinterpret_cast<const uint2*>(sv + i * 32 * W::kVBytes);
+            const uint2 w = *reinterpret_cast<const uint2*>(sv + i * 32 * F::kVBytes);
             v[i][0] = w.x; v[i][1] = w.y;
           }
         }
 #pragma unroll
-        for (int w = 0; w < W::kVBytes / 4; ++w) {
+        for (int w = 0; w < F::kVBytes / 4; ++w) {
           // bytes of two tokens side by side: entry 4 w + 2 x (+ 1) of tokens 2 t, 2 t + 1 and of the two 8 further on
 #pragma unroll
           for (int x = 0; x < 2; ++x) {
@@ -465,97 +575,145 @@ attend_split_kernel(const __grid_constant__ AttendParams P, const T* __restrict_
       }
     }
     copy_wait<0>();
-
-    // ---- the warps' parts joined: relative to the CTA's largest logit of each row
 #pragma unroll
     for (int n = 0; n < kTiles; ++n)
 #pragma unroll
-      for (int i = 0; i < 2; ++i) {
+      for (int i = 0; i < 2; ++i)
 #pragma unroll
         for (int x = 4; x < 32; x <<= 1) sum[n][i] += __shfl_xor_sync(0xffffffffu, sum[n][i], x);
-        if (g == 0) {
-          s_stat[warp][8 * n + 2 * t + i][0] = top_s[n][i];
-          s_stat[warp][8 * n + 2 * t + i][1] = sum[n][i];
-        }
-      }
-    __syncthreads();                                 // (also: nobody reads the stages any more)
-    float* so = reinterpret_cast<float*>(smem);      // [warp][row][kPitch]
-#pragma unroll
-    for (int n = 0; n < kTiles; ++n)
-#pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        const int row = 8 * n + 2 * t + i;
-        float m = s_stat[0][row][0];
-#pragma unroll
-        for (int w = 1; w < kWarps; ++w) m = fmaxf(m, s_stat[w][row][0]);
-        const float r = ex2(top_v[n][i] - kLift - m);
-        float* dst = so + (warp * kRowsTile + row) * kPitch + 4 * g;
-        // four entries of the lane's kD / 8 at a time: place 8 k + g of the row holds entries (kD / 8) g + 4 k ..
-#pragma unroll
-        for (int k = 0; k < kSteps / 2; ++k)
-          *reinterpret_cast<float4*>(dst + 32 * k) =
-              make_float4(o[n][2 * k][i] * r, o[n][2 * k][2 + i] * r, o[n][2 * k + 1][i] * r, o[n][2 * k + 1][2 + i] * r);
-      }
-    __syncthreads();
-    const long long slot = (long long)blockIdx.x + (long long)unit * P.row_tiles + rt;
-    for (int i = tid; i < kRowsTile * (kD / 4); i += kAttThreads) {
-      const int row = i / (kD / 4), x = i - row * (kD / 4);
-      float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll
-      for (int w = 0; w < kWarps; ++w) {
-        const float4 y = *reinterpret_cast<const float4*>(so + (w * kRowsTile + row) * kPitch + 4 * x);
-        a.x += y.x; a.y += y.y; a.z += y.z; a.w += y.w;
-      }
-      *reinterpret_cast<float4*>(P.part_o + (slot * kRowsTile + row) * kD + 4 * x) = a;
-    }
-    if (tid < kRowsTile) {
-      float m = s_stat[0][tid][0], l = 0.f;
-      for (int w = 1; w < kWarps; ++w) m = fmaxf(m, s_stat[w][tid][0]);
-      for (int w = 0; w < kWarps; ++w) l += s_stat[w][tid][1] * ex2(s_stat[w][tid][0] - m);
-      P.part_ml[slot * kRowsTile + tid] = make_float2(m, l);
-    }
+    const long long slot = (long long)blockIdx.x * kWarps + (together ? 0 : warp) + (long long)unit * P.row_tiles + rt;
 
-    at = before + upto;
-    if (at >= end) break;
+    if (!together) {
+      // ---- this warp's part as it is.  Four entries of the lane's kD / 8 at a time: place 8 k + g of a row holds entries
+      // (kD / 8) g + 4 k ..
+#pragma unroll
+      for (int n = 0; n < kTiles; ++n)
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          const int row = 8 * n + 2 * t + i;
+          if (row < live_rows) {
+            const float r = ex2(top_v[n][i] - kLift - top_s[n][i]);
+            float* dst = P.part_o + (slot * kRows + row) * kD + 4 * g;
+#pragma unroll
+            for (int k = 0; k < kSteps / 2; ++k)
+              *reinterpret_cast<float4*>(dst + 32 * k) =
+                  make_float4(o[n][2 * k][i] * r, o[n][2 * k][2 + i] * r, o[n][2 * k + 1][i] * r, o[n][2 * k + 1][2 + i] * r);
+            if (g == 0) P.part_ml[slot * kRows + row] = make_float2(top_s[n][i], sum[n][i]);
+          }
+        }
+    } else {
+      // ---- the warps' parts joined: relative to the CTA's largest logit of each row
+      if (g == 0) {
+#pragma unroll
+        for (int n = 0; n < kTiles; ++n)
+#pragma unroll
+          for (int i = 0; i < 2; ++i) {
+            s_stat[warp][8 * n + 2 * t + i][0] = top_s[n][i];
+            s_stat[warp][8 * n + 2 * t + i][1] = sum[n][i];
+          }
+      }
+      __syncthreads();                                 // (also: nobody reads the stages any more)
+      float* so = reinterpret_cast<float*>(smem);      // [warp][row][kPitch]
+#pragma unroll
+      for (int n = 0; n < kTiles; ++n)
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          const int row = 8 * n + 2 * t + i;
+          float m = s_stat[0][row][0];
+#pragma unroll
+          for (int w = 1; w < kWarps; ++w) m = fmaxf(m, s_stat[w][row][0]);
+          const float r = ex2(top_v[n][i] - kLift - m);
+          float* dst = so + (warp * kRows + row) * kPitch + 4 * g;
+#pragma unroll
+          for (int k = 0; k < kSteps / 2; ++k)
+            *reinterpret_cast<float4*>(dst + 32 * k) =
+                make_float4(o[n][2 * k][i] * r, o[n][2 * k][2 + i] * r, o[n][2 * k + 1][i] * r, o[n][2 * k + 1][2 + i] * r);
+        }
+      __syncthreads();
+      for (int i = tid; i < live_rows * (kD / 4); i += kThreads) {
+        const int row = i / (kD / 4), x = i - row * (kD / 4);
+        float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+        for (int w = 0; w < kWarps; ++w) {
+          const float4 y = *reinterpret_cast<const float4*>(so + (w * kRows + row) * kPitch + 4 * x);
+          a.x += y.x; a.y += y.y; a.z += y.z; a.w += y.w;
+        }
+        *reinterpret_cast<float4*>(P.part_o + (slot * kRows + row) * kD + 4 * x) = a;
+      }
+      if (tid < live_rows) {
+        float m = s_stat[0][tid][0], l = 0.f;
+        for (int w = 1; w < kWarps; ++w) m = fmaxf(m, s_stat[w][tid][0]);
+        for (int w = 0; w < kWarps; ++w) l += s_stat[w][tid][1] * ex2(s_stat[w][tid][0] - m);
+        P.part_ml[slot * kRows + tid] = make_float2(m, l);
+      }
+    }
+    }                                                  // (hi > lo)
+
+    if (together) return;
+    at = upto;
+    if (at >= end) return;
     // the next row tile, or the next head that holds tokens
     before += n_gran;
     if (++rt == P.row_tiles) {
       rt = 0;
-      do ++unit; while (granules(P, unit) == 0);     // (one is left: at < end <= total)
+      do len = c.length(++unit); while (len == 0);     // (one is left: at < end <= total)
+      n_gran = granules(len);
     }
-    __syncthreads();                                 // the shared memory is free again
   }
 }
 
-// Parts of row tile (unit, rt): slots first .. last, or none (last < first).
+// The parts of a row tile: up to three runs of slots, of the warps of its first CTA, of whole CTAs, of the warps of its last.
 struct Parts {
-  long long first, last;
+  long long slot[3];
+  int n[3], step1;                                     // the middle run's slots lie step1 apart
+  __device__ __forceinline__ int count() const { return n[0] + n[1] + n[2]; }
+  __device__ __forceinline__ long long operator[](int i) const {
+    return i < n[0] ? slot[0] + i : i < n[0] + n[1] ? slot[1] + (long long)(i - n[0]) * step1 : slot[2] + (i - n[0] - n[1]);
+  }
 };
 
-__device__ __forceinline__ Parts parts_of(const AttendParams& P, int unit, int rt, long long before, long long total) {
-  const long long n = granules(P, unit);
-  Parts r{0, -1};
+__device__ __forceinline__ Parts parts_of(const AttendParams& P, int unit, int rt) {
+  Parts r{};
+  r.step1 = P.warps;
+  const long long b = P.before[unit], n = P.before[unit + 1] - b;
   if (n == 0) return r;
-  const int ctas = sharers(P, total);
-  const long long u = (long long)unit * P.row_tiles + rt, t0 = before * P.row_tiles + rt * n;
-  r.first = ((t0 + 1) * ctas - 1) / total + u;
-  r.last = ((t0 + n) * ctas - 1) / total + u;
+  const Shares ctas(P.before[P.c.units()] * P.row_tiles, P.ctas);
+  const long long u = (long long)unit * P.row_tiles + rt, v0 = b * P.row_tiles + rt * n, v1 = v0 + n;
+  const int c0 = ctas.of(v0 + kSetup), c1 = ctas.of(v1 - 1);
+  int mid0 = c0, mid1 = c1;                            // CTAs that lie wholly inside
+  for (int side = 0; side < 2; ++side) {
+    const int cta = side == 0 ? c0 : c1;
+    const long long s0 = ctas.begin(cta), s1 = ctas.begin(cta + 1);
+    if ((side == 1 && c1 == c0) || (v0 <= s0 && s1 <= v1)) continue;
+    const Shares pieces(s1 - s0, P.warps);
+    const long long from = max(v0 + kSetup, s0) - s0, to = min(v1, s1) - s0;
+    const int w0 = pieces.of(from), w1 = pieces.of(to - 1);
+    r.slot[side == 0 ? 0 : 2] = (long long)cta * P.warps + w0 + u;
+    r.n[side == 0 ? 0 : 2] = w1 - w0 + 1;
+    if (side == 0) mid0 = c0 + 1; else mid1 = c1 - 1;
+  }
+  r.slot[1] = (long long)mid0 * P.warps + u;
+  r.n[1] = max(mid1 - mid0 + 1, 0);
   return r;
 }
 
 // One warp: the largest logit of a row over its parts, and the sum of 2^(logit - it).
 __device__ __forceinline__ float2 join_stats(const AttendParams& P, const Parts& r, int row) {
-  const int lane = threadIdx.x & 31;
+  const int lane = threadIdx.x & 31, n = r.count();
   float m = kNone, l = 0.f;
-  for (long long s = r.first + lane; s <= r.last; s += 32) m = fmaxf(m, P.part_ml[s * P.tile_rows + row].x);
-#pragma unroll
-  for (int x = 1; x < 32; x <<= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, x));
-  for (long long s = r.first + lane; s <= r.last; s += 32) {
-    const float2 a = P.part_ml[s * P.tile_rows + row];
-    l += a.y * ex2(a.x - m);
+  for (int i = lane; i < n; i += 32) {                 // (a running sum: each part is read once)
+    const float2 a = P.part_ml[r[i] * P.tile_rows + row];
+    const float top = fmaxf(m, a.x);
+    l = l * ex2(m - top) + a.y * ex2(a.x - top);
+    m = top;
   }
 #pragma unroll
-  for (int x = 1; x < 32; x <<= 1) l += __shfl_xor_sync(0xffffffffu, l, x);
+  for (int x = 1; x < 32; x <<= 1) {
+    const float m2 = __shfl_xor_sync(0xffffffffu, m, x), l2 = __shfl_xor_sync(0xffffffffu, l, x);
+    const float top = fmaxf(m, m2);
+    l = l * ex2(m - top) + l2 * ex2(m2 - top);
+    m = top;
+  }
   return make_float2(m, l);
 }
 
@@ -564,7 +722,6 @@ template <typename T, int kD>
 __global__ void __launch_bounds__(kJoinThreads)
 attend_join_kernel(const __grid_constant__ AttendParams P, const int32_t* __restrict__ row_counts, T* __restrict__ out,
                    float* __restrict__ lse, const float* weight_in, float* weight_out, int chunks) {
-  __shared__ long long s_sum[2][kJoinThreads / 32];
   __shared__ float s_lse[kMaxRows];
   __shared__ float4 s_o[kJoinThreads / 32][32];
   grid_dependency_wait();
@@ -576,23 +733,6 @@ attend_join_kernel(const __grid_constant__ AttendParams P, const int32_t* __rest
   const long long len = c.length(unit);
   const long long tok0 = is_row ? 0 : (long long)(job - unit * chunks) * kJoinTokens;
   if (!is_row && tok0 >= len) return;
-  // granules before this unit, and all of them
-  long long before = 0, total = 0;
-  for (int u = tid; u < units; u += kJoinThreads) {
-    const int n = granules(P, u);
-    total += n;
-    if (u < unit) before += n;
-  }
-#pragma unroll
-  for (int x = 1; x < 32; x <<= 1) {
-    before += __shfl_xor_sync(0xffffffffu, before, x);
-    total += __shfl_xor_sync(0xffffffffu, total, x);
-  }
-  if (lane == 0) { s_sum[0][warp] = before; s_sum[1][warp] = total; }
-  __syncthreads();
-  before = 0; total = 0;
-  for (int w = 0; w < kJoinThreads / 32; ++w) { before += s_sum[0][w]; total += s_sum[1][w]; }
-  total *= P.row_tiles;
   const int b = unit / c.Hkv, h = unit - b * c.Hkv;
   const int rows = row_count(P, row_counts, b);
 
@@ -600,14 +740,15 @@ attend_join_kernel(const __grid_constant__ AttendParams P, const int32_t* __rest
     const int r = job - unit * P.live, rr = P.row0 + r, rt = r / P.tile_rows, row = r - rt * P.tile_rows;
     const int m = rr % P.rows, j = h * P.G + rr / P.rows;
     if (m >= rows) return;                           // a row that the sequence has not got
-    const Parts parts = parts_of(P, unit, rt, before, total);
+    const Parts parts = parts_of(P, unit, rt);
     const float2 ml = join_stats(P, parts, row);     // (every warp for itself)
     constexpr int kLanes = kD / 4;                   // lanes of a part's row, 16 bytes each
     constexpr int kPer = 32 / kLanes;                // parts a warp reads side by side
     const int x = lane % kLanes;
     float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll 4
-    for (long long s = parts.first + warp * kPer + lane / kLanes; s <= parts.last; s += kPer * (kJoinThreads / 32)) {
+    for (int i = warp * kPer + lane / kLanes; i < parts.count(); i += kPer * (kJoinThreads / 32)) {
+      const long long s = parts[i];
       const float4 y = *reinterpret_cast<const float4*>(P.part_o + (s * P.tile_rows + row) * kD + 4 * x);
       const float f = ex2(P.part_ml[s * P.tile_rows + row].x - ml.x);
       a.x += y.x * f; a.y += y.y * f; a.z += y.z * f; a.w += y.w * f;
@@ -641,7 +782,7 @@ attend_join_kernel(const __grid_constant__ AttendParams P, const int32_t* __rest
   // ---- weights: the logits' log-sum-exps, then the tokens
   for (int r = warp; r < P.live; r += kJoinThreads / 32) {
     const int rt = r / P.tile_rows;
-    const float2 ml = join_stats(P, parts_of(P, unit, rt, before, total), r - rt * P.tile_rows);
+    const float2 ml = join_stats(P, parts_of(P, unit, rt), r - rt * P.tile_rows);
     if (lane == 0) s_lse[r] = ml.y > 0.f && (P.row0 + r) % P.rows < rows ? ml.x + log2f(ml.y) : INFINITY;     // (infinity: weighs nothing)
   }
   __syncthreads();
@@ -673,6 +814,7 @@ kvc_status resolve_attend(const kvc_cache* cache, const kvc_attend_desc* d, Atte
   KVC_REQUIRE8(d->causal == 0 || d->causal == 1, KVC_ERR_INVALID_ARG, "causal must be 0 or 1");
   KVC_REQUIRE8(d->reserved_ == 0, KVC_ERR_INVALID_ARG, "reserved_ must be 0");
   KVC_REQUIRE8(isfinite(d->scale), KVC_ERR_INVALID_ARG, "scale is not finite");
+  KVC_REQUIRE8(P->c.st[2] < (1LL << 31), KVC_ERR_UNSUPPORTED, "tokens of the cache lie 2^31 bytes or more apart");
   P->Hq = d->n_q_heads; P->G = d->n_q_heads / P->c.Hkv; P->rows = d->rows; P->causal = d->causal;
   P->scale = d->scale > 0.f ? d->scale : 1.0f / sqrtf((float)P->c.d);
   const int eb = d->dtype == KVC_F32 ? 4 : 2;
@@ -680,47 +822,53 @@ kvc_status resolve_attend(const kvc_cache* cache, const kvc_attend_desc* d, Atte
   return resolve_strides(d->out_stride, P->c.Bt, P->Hq, P->rows, P->c.d, eb, true, "out_stride", P->os);
 }
 
-// Query rows of a KV head in one launch: tiles of 8, or of 16 where there are more (the codes' conversion is shared).
-int tile_rows_of(int live) { return live <= 8 ? 8 : 16; }
+// Query rows that share the codes' conversion: 8, 16 or, in bf16, 32 (fp32 keeps twice the operands).
+int tile_rows_of(int live, int dtype) { return live <= 8 ? 8 : live <= 16 || dtype == KVC_F32 ? 16 : 32; }
 
 struct AttendLayout {
   int live, tile_rows, row_tiles, logit_rows;
-  size_t o, ml, logits, total;
+  size_t o, ml, before, logits, total;
 };
 
-AttendLayout attend_layout(const AttendParams& P, bool with_weight) {
+AttendLayout attend_layout(const AttendParams& P, int dtype, bool with_weight) {
   AttendLayout y;
   const long long all = (long long)P.G * P.rows;
   y.live = (int)(all < kMaxRows ? all : kMaxRows);
-  y.tile_rows = tile_rows_of(y.live);
+  y.tile_rows = tile_rows_of(y.live, dtype);
   y.row_tiles = (y.live + y.tile_rows - 1) / y.tile_rows;
   y.logit_rows = 2;
   while (y.logit_rows < y.live && y.logit_rows < y.tile_rows) y.logit_rows *= 2;
-  const size_t slots = (size_t)kMaxCtas + (size_t)P.c.units() * y.row_tiles;
+  const size_t slots = (size_t)kMaxCtas * kMaxWarps + (size_t)P.c.units() * y.row_tiles;
   y.o = 0;
   y.ml = align_up(slots * y.tile_rows * P.c.d * sizeof(float));
-  y.logits = y.ml + align_up(slots * y.tile_rows * sizeof(float2));
+  y.before = y.ml + align_up(slots * y.tile_rows * sizeof(float2));
+  y.logits = y.before + align_up(((size_t)P.c.units() + 1) * sizeof(long long));
   y.total = y.logits + (with_weight ? align_up((size_t)P.c.units() * y.row_tiles * P.c.cap * y.logit_rows * sizeof(float)) : 0);
   return y;
 }
 
 template <typename T, int kFormat, int kD, int kTiles, bool kWeight>
-kvc_status launch_split(const AttendParams& P, const T* q, const int32_t* row_counts, cudaStream_t st) {
-  using W = Warp<kFormat, kD, kTiles, sizeof(T) == 4, kWeight>;
+kvc_status launch_split(AttendParams& P, const T* q, const int32_t* row_counts, cudaStream_t st) {
+  using F = Form<T, kD, kTiles>;
+  static_assert(F::kWarps <= kMaxWarps && F::kSmem <= 220 * 1024, "shared memory and slots");
   auto kernel = attend_split_kernel<T, kFormat, kD, kTiles, kWeight>;
-  constexpr int stages = kWarps * W::kStages * W::kStageBytes, join = kWarps * 8 * kTiles * (kD + 4) * (int)sizeof(float);
-  constexpr int smem = stages > join ? stages : join;
-  KVC_CUDA(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
-  KVC_CUDA(launch_dependent(kernel, dim3(P.ctas), dim3(kAttThreads), smem, st, P, q, row_counts));
+  P.warps = F::kWarps;
+  KVC_CUDA(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, F::kSmem));
+  KVC_CUDA(launch_dependent(kernel, dim3(P.ctas), dim3(F::kThreads), F::kSmem, st, P, q, row_counts));
   KVC_LAUNCH_CHECK("attend_split_kernel");
   return KVC_OK;
 }
 
 template <typename T, int kFormat, int kD>
-kvc_status launch_split_form(const AttendParams& P, bool weight, const T* q, const int32_t* row_counts, cudaStream_t st) {
+kvc_status launch_split_form(AttendParams& P, bool weight, const T* q, const int32_t* row_counts, cudaStream_t st) {
   if (P.tile_rows == 8)
     return weight ? launch_split<T, kFormat, kD, 1, true>(P, q, row_counts, st) : launch_split<T, kFormat, kD, 1, false>(P, q, row_counts, st);
-  return weight ? launch_split<T, kFormat, kD, 2, true>(P, q, row_counts, st) : launch_split<T, kFormat, kD, 2, false>(P, q, row_counts, st);
+  if (P.tile_rows == 16)
+    return weight ? launch_split<T, kFormat, kD, 2, true>(P, q, row_counts, st) : launch_split<T, kFormat, kD, 2, false>(P, q, row_counts, st);
+  if constexpr (sizeof(T) == 2)
+    return weight ? launch_split<T, kFormat, kD, 4, true>(P, q, row_counts, st) : launch_split<T, kFormat, kD, 4, false>(P, q, row_counts, st);
+  set_error("no form of attend_split_kernel for tiles of %d rows", P.tile_rows);
+  return KVC_ERR_UNSUPPORTED;
 }
 
 template <typename T>
@@ -761,7 +909,7 @@ kvc_status kvc_attend_workspace_size(const kvc_cache* cache, const kvc_attend_de
   const kvc_status s = resolve_attend(cache, desc, &P);
   if (s != KVC_OK) return s;
   KVC_REQUIRE8(bytes != nullptr, KVC_ERR_INVALID_ARG, "bytes is NULL");
-  *bytes = attend_layout(P, with_weight != 0).total;
+  *bytes = attend_layout(P, desc->dtype, with_weight != 0).total;
   return KVC_OK;
 }
 
@@ -772,7 +920,7 @@ kvc_status kvc_attend(const kvc_cache* cache, const kvc_attend_desc* desc, const
   if (s != KVC_OK) return s;
   KVC_REQUIRE8(q && out && aligned16(q) && aligned16(out), KVC_ERR_INVALID_ARG, "q or out is NULL or not 16-byte aligned");
   KVC_REQUIRE8(weight_in == nullptr || weight_out != nullptr, KVC_ERR_INVALID_ARG, "weight_in without weight_out");
-  const AttendLayout y = attend_layout(P, weight_out != nullptr);
+  const AttendLayout y = attend_layout(P, desc->dtype, weight_out != nullptr);
   KVC_REQUIRE8(workspace != nullptr, KVC_ERR_WORKSPACE, "workspace is NULL (%zu bytes needed)", y.total);
   KVC_REQUIRE8((reinterpret_cast<uintptr_t>(workspace) & 255u) == 0, KVC_ERR_WORKSPACE, "workspace is not 256-byte aligned");
   KVC_REQUIRE8(workspace_bytes >= y.total, KVC_ERR_WORKSPACE, "workspace has %zu bytes, %zu needed", workspace_bytes, y.total);
@@ -784,6 +932,7 @@ kvc_status kvc_attend(const kvc_cache* cache, const kvc_attend_desc* desc, const
   P.tile_rows = y.tile_rows; P.logit_rows = y.logit_rows;
   P.part_o = (float*)((char*)workspace + y.o);
   P.part_ml = (float2*)((char*)workspace + y.ml);
+  P.before = (long long*)((char*)workspace + y.before);
   P.logits = (float*)((char*)workspace + y.logits);
   return desc->dtype == KVC_F32 ? run_attend<float>(P, y, (const float*)q, row_counts, (float*)out, lse, weight_in, weight_out, (cudaStream_t)stream)
                                 : run_attend<__nv_bfloat16>(P, y, (const __nv_bfloat16*)q, row_counts, (__nv_bfloat16*)out, lse, weight_in,
