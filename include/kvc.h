@@ -327,20 +327,26 @@ KVC_API kvc_status kvc_scale(float* x, int64_t n, float factor, void* stream);
  * Angles are formed in 64 bits: at position 2^31 they are still within 1e-6. */
 typedef enum { KVC_ROPE_NONE = 0, KVC_ROPE_LINEAR = 1, KVC_ROPE_BANDED = 2, KVC_ROPE_YARN = 3 } kvc_rope_scaling;
 
+/* The pairs' frequencies, made once by kvc_rope_init and used by any number of calls (host memory, plain data). */
+typedef struct {
+  int32_t rot_dim;     /* a multiple of 16, 16 <= rot_dim <= 128 */
+  int32_t interleaved; /* 0: halves, 1: neighbours */
+  double mscale;       /* m */
+  double turn[64];     /* f_i / 2pi */
+} kvc_rope;
+
+/* theta > 1.  factor >= 1 is used with scaling only; original_ctx > 0 and 0 < turns_low < turns_high by KVC_ROPE_BANDED
+ * and KVC_ROPE_YARN only.  mscale > 0 sets m, 0 takes the scaling's own (1 but for YARN). */
+KVC_API kvc_status kvc_rope_init(kvc_rope* rope, int32_t rot_dim, int32_t interleaved, double theta, int32_t scaling,
+                                 double factor, double turns_low, double turns_high, double original_ctx, double mscale);
+
 typedef struct {
   int32_t batch, n_q_heads, n_kv_heads; /* q [batch, n_q_heads, rows, head_dim], k [batch, n_kv_heads, rows, head_dim] */
-  int32_t head_dim;                     /* 64 or 128 */
+  int32_t head_dim;                     /* 64 or 128, >= rot_dim */
   int32_t rows;                         /* >= 1 */
-  int32_t rot_dim;                      /* a multiple of 16, 16 <= rot_dim <= head_dim */
   int32_t dtype;                        /* kvc_dtype of q, k and the outputs */
-  int32_t interleaved;                  /* 0: halves, 1: neighbours */
   int32_t inverse;                      /* 1: turns by -p f_i (the gradient of the forward turn, as m stays) */
-  int32_t scaling;                      /* kvc_rope_scaling */
-  double theta;                         /* > 1 */
-  double factor;                        /* >= 1; used with scaling only, as are the three below */
-  double turns_low, turns_high;         /* 0 < turns_low < turns_high (BANDED, YARN) */
-  double original_ctx;                  /* > 0 (BANDED, YARN) */
-  double mscale;                        /* m; 0: as above (1 without YARN) */
+  int32_t reserved_;                    /* must be 0 */
   int64_t q_stride[3], k_stride[3];     /* element strides (batch, head, row) of q, k, as in kvc_desc; 0 in slot 0: dense */
   int64_t q_out_stride[3], k_out_stride[3];
 } kvc_rope_desc;
@@ -348,8 +354,8 @@ typedef struct {
 /* positions: int64, position of row r of sequence b at [b * pos_stride + r] (pos_stride 0: the same for all
  * sequences); may be negative.  q or k (with its output) may be NULL.  An output may be its input (same
  * pointer and strides); other overlaps are not allowed. */
-KVC_API kvc_status kvc_rotary(const kvc_rope_desc* desc, const void* q, const void* k, const int64_t* positions,
-                              int64_t pos_stride, void* q_out, void* k_out, void* stream);
+KVC_API kvc_status kvc_rotary(const kvc_rope* rope, const kvc_rope_desc* desc, const void* q, const void* k,
+                              const int64_t* positions, int64_t pos_stride, void* q_out, void* k_out, void* stream);
 
 /*
  * A cache held in 8 bits.  `block` tokens of a head share an exponent, K and V apart: a value is

@@ -54,12 +54,14 @@ class KvcAttendDesc(C.Structure):
     ]
 
 
+class KvcRope(C.Structure):
+    _fields_ = [("rot_dim", C.c_int32), ("interleaved", C.c_int32), ("mscale", C.c_double), ("turn", C.c_double * 64)]
+
+
 class KvcRopeDesc(C.Structure):
     _fields_ = [
         ("batch", C.c_int32), ("n_q_heads", C.c_int32), ("n_kv_heads", C.c_int32), ("head_dim", C.c_int32),
-        ("rows", C.c_int32), ("rot_dim", C.c_int32), ("dtype", C.c_int32), ("interleaved", C.c_int32),
-        ("inverse", C.c_int32), ("scaling", C.c_int32), ("theta", C.c_double), ("factor", C.c_double),
-        ("turns_low", C.c_double), ("turns_high", C.c_double), ("original_ctx", C.c_double), ("mscale", C.c_double),
+        ("rows", C.c_int32), ("dtype", C.c_int32), ("inverse", C.c_int32), ("reserved_", C.c_int32),
         ("q_stride", C.c_int64 * 3), ("k_stride", C.c_int64 * 3), ("q_out_stride", C.c_int64 * 3),
         ("k_out_stride", C.c_int64 * 3),
     ]
@@ -133,14 +135,16 @@ def _load():
     lib.kvc_compress.argtypes = [dp, vp, vp, vp, i64, vp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
     lib.kvc_compress.restype = C.c_int
     cp, ap = C.POINTER(KvcCache), C.POINTER(KvcAttendDesc)
-    lib.kvc_rotary.argtypes = [C.POINTER(KvcRopeDesc), vp, vp, vp, i64, vp, vp, vp]
+    f64 = C.c_double
+    lib.kvc_rope_init.argtypes = [C.POINTER(KvcRope), i32, i32, f64, i32, f64, f64, f64, f64, f64]
+    lib.kvc_rotary.argtypes = [C.POINTER(KvcRope), C.POINTER(KvcRopeDesc), vp, vp, vp, i64, vp, vp, vp]
     lib.kvc_cache_gather.argtypes = [dp, vp, vp, vp, vp, i32, cp, vp, vp]
     lib.kvc_cache_append.argtypes = [cp, vp, vp, i32, i32, C.POINTER(i64), vp, vp, vp, vp, vp]
     lib.kvc_cache_read.argtypes = [cp, vp, i64, i32, vp, vp, vp]
     lib.kvc_attend_workspace_size.argtypes = [cp, ap, i32, C.POINTER(sz)]
     lib.kvc_attend.argtypes = [cp, ap, vp, vp, vp, vp, vp, vp, vp, sz, vp]
     lib.kvc_evict.argtypes = [cp, cp, vp, i64, i64, vp, vp, vp]
-    for name in ("rotary", "cache_gather", "cache_append", "cache_read", "attend_workspace_size", "attend", "evict"):
+    for name in ("rope_init", "rotary", "cache_gather", "cache_append", "cache_read", "attend_workspace_size", "attend", "evict"):
         getattr(lib, "kvc_" + name).restype = C.c_int
     lib.kvc_last_error.restype = C.c_char_p
     lib.kvc_launch_count.argtypes = [i32]

@@ -115,39 +115,10 @@ rotary_kernel(const __grid_constant__ RotaryParams P, const T* q, const T* k, co
   }
 }
 
-// Angle per position of every pair over 2pi, in 64 bits.
-void fill_turns(const kvc_rope_desc& D, RotaryParams* P) {
-  const double two_pi = 6.283185307179586476925286766559;
-  const double lt = log(D.theta);
-  double first = 0, last = 0;
-  if (D.scaling == KVC_ROPE_YARN) {
-    first = floor(D.rot_dim * log(D.original_ctx / (D.turns_high * two_pi)) / (2.0 * lt));
-    last = ceil(D.rot_dim * log(D.original_ctx / (D.turns_low * two_pi)) / (2.0 * lt));
-    if (first < 0) first = 0;
-    if (last > D.rot_dim - 1) last = D.rot_dim - 1;
-  }
-  for (int i = 0; i < D.rot_dim / 2; ++i) {
-    double f = pow(D.theta, -2.0 * i / D.rot_dim);
-    if (D.scaling == KVC_ROPE_LINEAR) {
-      f /= D.factor;
-    } else if (D.scaling == KVC_ROPE_BANDED) {
-      double keep = (D.original_ctx * f / two_pi - D.turns_low) / (D.turns_high - D.turns_low);
-      keep = keep < 0 ? 0 : (keep > 1 ? 1 : keep);
-      f = keep * f + (1.0 - keep) * f / D.factor;
-    } else if (D.scaling == KVC_ROPE_YARN) {
-      const double width = last - first > 0.001 ? last - first : 0.001;
-      double ramp = (i - first) / width;
-      ramp = ramp < 0 ? 0 : (ramp > 1 ? 1 : ramp);
-      f = (1.0 - ramp) * f + ramp * f / D.factor;
-    }
-    P->turn[i] = (D.inverse ? -f : f) / two_pi;
-  }
-}
-
 template <typename T>
-kvc_status launch_rotary(const kvc_rope_desc& D, const RotaryParams& P, dim3 grid, const void* q, const void* k,
+kvc_status launch_rotary(bool interleaved, const RotaryParams& P, dim3 grid, const void* q, const void* k,
                          const int64_t* positions, void* q_out, void* k_out, cudaStream_t st) {
-  auto kernel = D.interleaved ? rotary_kernel<T, true> : rotary_kernel<T, false>;
+  auto kernel = interleaved ? rotary_kernel<T, true> : rotary_kernel<T, false>;
   KVC_CUDA(launch_dependent(kernel, grid, dim3(kRotThreads), 0, st, P, (const T*)q, (const T*)k, positions, (T*)q_out, (T*)k_out));
   KVC_LAUNCH_CHECK("rotary_kernel");
   return KVC_OK;
@@ -158,32 +129,68 @@ kvc_status launch_rotary(const kvc_rope_desc& D, const RotaryParams& P, dim3 gri
 
 using namespace kvc;
 
-extern "C" kvc_status kvc_rotary(const kvc_rope_desc* D, const void* q, const void* k, const int64_t* positions, int64_t pos_stride,
-                                 void* q_out, void* k_out, void* stream) {
-  KVC_REQUIRE8(D != nullptr, KVC_ERR_INVALID_ARG, "desc is NULL");
+extern "C" {
+
+kvc_status kvc_rope_init(kvc_rope* R, int32_t rot_dim, int32_t interleaved, double theta, int32_t scaling, double factor,
+                         double turns_low, double turns_high, double original_ctx, double mscale) {
+  KVC_REQUIRE8(R != nullptr, KVC_ERR_INVALID_ARG, "rope is NULL");
+  KVC_REQUIRE8(rot_dim >= 16 && rot_dim <= 128 && rot_dim % 16 == 0, KVC_ERR_UNSUPPORTED, "rot_dim must be a multiple of 16 within [16, 128]");
+  KVC_REQUIRE8(interleaved == 0 || interleaved == 1, KVC_ERR_INVALID_ARG, "interleaved must be 0 or 1");
+  KVC_REQUIRE8(isfinite(theta) && theta > 1.0, KVC_ERR_INVALID_ARG, "theta must be finite and > 1");
+  KVC_REQUIRE8(scaling >= KVC_ROPE_NONE && scaling <= KVC_ROPE_YARN, KVC_ERR_INVALID_ARG, "unknown scaling");
+  KVC_REQUIRE8(scaling == KVC_ROPE_NONE || (isfinite(factor) && factor >= 1.0), KVC_ERR_INVALID_ARG, "factor must be finite and >= 1");
+  if (scaling == KVC_ROPE_BANDED || scaling == KVC_ROPE_YARN) {
+    KVC_REQUIRE8(isfinite(turns_high) && turns_low > 0 && turns_high > turns_low, KVC_ERR_INVALID_ARG, "0 < turns_low < turns_high is needed");
+    KVC_REQUIRE8(isfinite(original_ctx) && original_ctx > 0, KVC_ERR_INVALID_ARG, "original_ctx must be positive");
+  }
+  KVC_REQUIRE8(isfinite(mscale) && mscale >= 0, KVC_ERR_INVALID_ARG, "mscale must be finite and >= 0");
+  const double two_pi = 6.283185307179586476925286766559;
+  const double lt = log(theta);
+  double first = 0, last = 0;
+  if (scaling == KVC_ROPE_YARN) {
+    first = floor(rot_dim * log(original_ctx / (turns_high * two_pi)) / (2.0 * lt));
+    last = ceil(rot_dim * log(original_ctx / (turns_low * two_pi)) / (2.0 * lt));
+    if (first < 0) first = 0;
+    if (last > rot_dim - 1) last = rot_dim - 1;
+  }
+  for (int i = 0; i < 64; ++i) {
+    double f = i < rot_dim / 2 ? pow(theta, -2.0 * i / rot_dim) : 0.0;
+    if (scaling == KVC_ROPE_LINEAR) {
+      f /= factor;
+    } else if (scaling == KVC_ROPE_BANDED) {
+      double keep = (original_ctx * f / two_pi - turns_low) / (turns_high - turns_low);
+      keep = keep < 0 ? 0 : (keep > 1 ? 1 : keep);
+      f = keep * f + (1.0 - keep) * f / factor;
+    } else if (scaling == KVC_ROPE_YARN) {
+      const double width = last - first > 0.001 ? last - first : 0.001;
+      double ramp = (i - first) / width;
+      ramp = ramp < 0 ? 0 : (ramp > 1 ? 1 : ramp);
+      f = (1.0 - ramp) * f + ramp * f / factor;
+    }
+    R->turn[i] = f / two_pi;
+  }
+  R->rot_dim = rot_dim;
+  R->interleaved = interleaved;
+  R->mscale = mscale > 0 ? mscale : scaling == KVC_ROPE_YARN ? 0.1 * log(factor) + 1.0 : 1.0;
+  return KVC_OK;
+}
+
+kvc_status kvc_rotary(const kvc_rope* R, const kvc_rope_desc* D, const void* q, const void* k, const int64_t* positions, int64_t pos_stride,
+                      void* q_out, void* k_out, void* stream) {
+  KVC_REQUIRE8(R != nullptr && D != nullptr, KVC_ERR_INVALID_ARG, "rope or desc is NULL");
   KVC_REQUIRE8(D->batch >= 1 && D->rows >= 1, KVC_ERR_INVALID_ARG, "batch and rows must be >= 1");
   KVC_REQUIRE8(D->batch <= 65535, KVC_ERR_UNSUPPORTED, "batch > 65535");
   KVC_REQUIRE8(D->rows <= (1 << 30), KVC_ERR_UNSUPPORTED, "rows > 2^30");
   KVC_REQUIRE8(D->head_dim == 64 || D->head_dim == 128, KVC_ERR_UNSUPPORTED, "head_dim must be 64 or 128");
-  KVC_REQUIRE8(D->rot_dim >= 16 && D->rot_dim <= D->head_dim && D->rot_dim % 16 == 0, KVC_ERR_UNSUPPORTED,
-              "rot_dim must be a multiple of 16 within [16, head_dim]");
+  KVC_REQUIRE8(R->rot_dim >= 16 && R->rot_dim <= D->head_dim && R->rot_dim % 16 == 0, KVC_ERR_UNSUPPORTED,
+               "rot_dim must be a multiple of 16 within [16, head_dim]");
   kvc_status s = check_dtype(D->dtype);
   if (s != KVC_OK) return s;
-  KVC_REQUIRE8((D->interleaved == 0 || D->interleaved == 1) && (D->inverse == 0 || D->inverse == 1), KVC_ERR_INVALID_ARG,
-              "interleaved and inverse must be 0 or 1");
-  KVC_REQUIRE8(D->scaling >= KVC_ROPE_NONE && D->scaling <= KVC_ROPE_YARN, KVC_ERR_INVALID_ARG, "unknown scaling");
-  KVC_REQUIRE8(isfinite(D->theta) && D->theta > 1.0, KVC_ERR_INVALID_ARG, "theta must be finite and > 1");
-  KVC_REQUIRE8(D->scaling == KVC_ROPE_NONE || (isfinite(D->factor) && D->factor >= 1.0), KVC_ERR_INVALID_ARG,
-              "factor must be finite and >= 1");
-  if (D->scaling == KVC_ROPE_BANDED || D->scaling == KVC_ROPE_YARN) {
-    KVC_REQUIRE8(isfinite(D->turns_high) && D->turns_low > 0 && D->turns_high > D->turns_low, KVC_ERR_INVALID_ARG,
-                "0 < turns_low < turns_high is needed");
-    KVC_REQUIRE8(isfinite(D->original_ctx) && D->original_ctx > 0, KVC_ERR_INVALID_ARG, "original_ctx must be positive");
-  }
-  KVC_REQUIRE8(isfinite(D->mscale) && D->mscale >= 0, KVC_ERR_INVALID_ARG, "mscale must be finite and >= 0");
+  KVC_REQUIRE8(D->inverse == 0 || D->inverse == 1, KVC_ERR_INVALID_ARG, "inverse must be 0 or 1");
+  KVC_REQUIRE8(D->reserved_ == 0, KVC_ERR_INVALID_ARG, "reserved_ must be 0");
   KVC_REQUIRE8(q != nullptr || k != nullptr, KVC_ERR_INVALID_ARG, "q and k are both NULL");
   KVC_REQUIRE8((q == nullptr) == (q_out == nullptr) && (k == nullptr) == (k_out == nullptr), KVC_ERR_INVALID_ARG,
-              "q and q_out, k and k_out go together");
+               "q and q_out, k and k_out go together");
   KVC_REQUIRE8(positions != nullptr && pos_stride >= 0, KVC_ERR_INVALID_ARG, "positions is NULL or pos_stride negative");
   const void* ptrs[4] = {q, k, q_out, k_out};
   for (const void* p : ptrs) KVC_REQUIRE8(aligned16(p), KVC_ERR_INVALID_ARG, "q, k and the outputs must be 16-byte aligned");
@@ -192,17 +199,15 @@ extern "C" kvc_status kvc_rotary(const kvc_rope_desc* D, const void* q, const vo
   P.Hkv = k ? D->n_kv_heads : 0;
   KVC_REQUIRE8((!q || D->n_q_heads >= 1) && (!k || D->n_kv_heads >= 1), KVC_ERR_INVALID_ARG, "head counts must be >= 1");
   KVC_REQUIRE8(P.Hq <= kMaxQHeads && P.Hkv <= kMaxQHeads, KVC_ERR_UNSUPPORTED, "more than %d heads", kMaxQHeads);
-  P.d = D->head_dim; P.rows = D->rows; P.rot = D->rot_dim; P.pos_stride = pos_stride;
+  P.d = D->head_dim; P.rows = D->rows; P.rot = R->rot_dim; P.pos_stride = pos_stride;
   const int eb = D->dtype == KVC_F32 ? 4 : 2;
   if (q && (s = resolve_strides(D->q_stride, D->batch, P.Hq, P.rows, P.d, eb, false, "q_stride", P.qs)) != KVC_OK) return s;
-  if (q && (s = resolve_strides(D->q_out_stride, D->batch, P.Hq, P.rows, P.d, eb, true,
-                                "q_out_stride", P.qo)) != KVC_OK) return s;
+  if (q && (s = resolve_strides(D->q_out_stride, D->batch, P.Hq, P.rows, P.d, eb, true, "q_out_stride", P.qo)) != KVC_OK) return s;
   if (k && (s = resolve_strides(D->k_stride, D->batch, P.Hkv, P.rows, P.d, eb, false, "k_stride", P.ks)) != KVC_OK) return s;
-  if (k && (s = resolve_strides(D->k_out_stride, D->batch, P.Hkv, P.rows, P.d, eb, true,
-                                "k_out_stride", P.ko)) != KVC_OK) return s;
-  P.mscale = (float)(D->mscale > 0 ? D->mscale : D->scaling == KVC_ROPE_YARN ? 0.1 * log(D->factor) + 1.0 : 1.0);
+  if (k && (s = resolve_strides(D->k_out_stride, D->batch, P.Hkv, P.rows, P.d, eb, true, "k_out_stride", P.ko)) != KVC_OK) return s;
+  P.mscale = (float)R->mscale;
   if ((s = require_device()) != KVC_OK) return s;
-  fill_turns(*D, &P);
+  for (int i = 0; i < 64; ++i) P.turn[i] = D->inverse ? -R->turn[i] : R->turn[i];
 
   P.tile_rows = P.rows < kRotRows ? P.rows : kRotRows;
   const long long tiles = (P.rows + P.tile_rows - 1) / P.tile_rows;
@@ -215,6 +220,9 @@ extern "C" kvc_status kvc_rotary(const kvc_rope_desc* D, const void* q, const vo
     if (P.heads_per_cta > heads) P.heads_per_cta = heads;
   }
   const dim3 grid((unsigned)tiles, D->batch, (heads + P.heads_per_cta - 1) / P.heads_per_cta);
-  return D->dtype == KVC_F32 ? launch_rotary<float>(*D, P, grid, q, k, positions, q_out, k_out, (cudaStream_t)stream)
-                             : launch_rotary<__nv_bfloat16>(*D, P, grid, q, k, positions, q_out, k_out, (cudaStream_t)stream);
+  const bool il = R->interleaved != 0;
+  return D->dtype == KVC_F32 ? launch_rotary<float>(il, P, grid, q, k, positions, q_out, k_out, (cudaStream_t)stream)
+                             : launch_rotary<__nv_bfloat16>(il, P, grid, q, k, positions, q_out, k_out, (cudaStream_t)stream);
 }
+
+}  // extern "C"

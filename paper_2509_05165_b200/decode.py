@@ -1,7 +1,9 @@
 """Decoding from a compressed cache: the binding of kvc.h's 8-bit cache, its attention and eviction, and rotary positions.
 
 Same names as the C entry points; tensors are checked for type, shape, layout and device here, values and sizes in the
-library.  Everything runs on ``stream`` (default: the current one), which has to be a stream of the tensors' device, and
+library.  A decoding step makes several calls per layer whose kernels take microseconds, so what a combination of types,
+shapes, strides and devices was checked for and turned into is kept (by these, never by a tensor's identity or address) with
+the object that the calls share, and looked up by the next call.  Everything runs on ``stream`` (default: the current one), which has to be a stream of the tensors' device, and
 that device the current one.
 
     cache = kvc.alloc_cache(batch, n_kv_heads, head_dim, capacity, device=dev)      # one layer
@@ -19,7 +21,7 @@ from typing import Optional, Sequence
 
 import torch
 
-from .binding import (BF16, F32, KvcAttendDesc, KvcCache, KvcError, KvcRopeDesc, _check, _dptr, _load, _ptr_array, _stream, _ws)
+from .binding import BF16, F32, KvcAttendDesc, KvcCache, KvcError, KvcRope, KvcRopeDesc, _check, _load, _ptr_array, _stream
 
 INT8, E4M3 = 0, 1
 _SCALING = {"none": 0, "linear": 1, "banded": 2, "yarn": 3}
@@ -56,14 +58,46 @@ def _dense(t: Optional[torch.Tensor], name: str, dtype, *shape) -> None:
     _refuse(not t.is_contiguous(), "%s must be contiguous", name)
 
 
-def _one_device(first: torch.Tensor, *others: Optional[torch.Tensor]) -> None:
-    """All tensors on one device, and that the current one (a launch goes to the current device)."""
+def _sig(t: Optional[torch.Tensor]):
+    """All that the checks go by."""
+    return None if t is None else (t.shape, t.stride(), t.dtype, t.get_device())
+
+
+class _Plans(dict):
+    """What calls with the same signature share; forgotten when there are very many of them."""
+
+    def keep(self, key, plan):
+        if len(self) >= 512:
+            self.clear()
+        self[key] = plan
+        return plan
+
+
+def _one_device(first: torch.Tensor, *others: Optional[torch.Tensor]) -> int:
     dev = first.get_device()
     for t in others:
         if t is not None and t.get_device() != dev:
             raise KvcError(-1, "tensors on different devices: %s and %s" % (first.device, t.device))
-    if dev >= 0 and dev != torch.cuda.current_device():
-        raise KvcError(-1, "tensors on %s, which is not the current device" % (first.device,))
+    return dev
+
+
+_get_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+
+
+def _launch_stream(dev: int, stream):
+    """The stream to launch on; the tensors' device has to be the current one (launches go there)."""
+    if dev < 0:
+        return _stream(stream)
+    if dev != _get_device():
+        raise KvcError(-1, "tensors on cuda:%d, which is not the current device" % dev)
+    if stream is None and _raw_stream is not None:
+        return _raw_stream(dev)
+    return _stream(stream)
+
+
+def _ptr(t: Optional[torch.Tensor]):
+    return None if t is None else t.data_ptr()
 
 
 def _strides(t: torch.Tensor):
@@ -106,6 +140,7 @@ class Cache:
         self.batch, self.n_kv_heads, self.capacity, self.head_dim, self.format = b, h, cap, d, fmt
         self.struct = KvcCache(b, h, d, block, fmt, 0, cap, ks, k.data_ptr(), v.data_ptr(), k_exp.data_ptr(), v_exp.data_ptr(),
                                lengths.data_ptr())
+        self.ref, self.plans = C.byref(self.struct), _Plans()
 
     @property
     def bytes(self) -> int:
@@ -121,7 +156,7 @@ def alloc_cache(batch: int, n_kv_heads: int, head_dim: int, capacity: int, block
 
 @dataclasses.dataclass(frozen=True)
 class Rotary:
-    """Rotary positions of ``rot_dim`` of a head's entries; see ``kvc_rope_desc`` for the scalings."""
+    """Rotary positions of ``rot_dim`` of a head's entries; see ``kvc_rope_scaling`` for the scalings."""
     rot_dim: int
     theta: float = 10000.0
     interleaved: bool = False
@@ -132,20 +167,23 @@ class Rotary:
     original_ctx: float = 8192.0
     mscale: float = 0.0              # 0: the scaling's own
 
+    def __post_init__(self):
+        _refuse(self.scaling not in _SCALING, "unknown scaling %r", self.scaling)
+        rope = KvcRope()
+        _check(_load().kvc_rope_init(C.byref(rope), self.rot_dim, int(self.interleaved), self.theta, _SCALING[self.scaling], self.factor,
+                                     self.turns_low, self.turns_high, self.original_ctx, self.mscale))
+        object.__setattr__(self, "struct", rope)
+        object.__setattr__(self, "ref", C.byref(rope))
+        object.__setattr__(self, "plans", _Plans())
 
-def kvc_rotary(rope: Rotary, q: Optional[torch.Tensor], k: Optional[torch.Tensor], positions: torch.Tensor,
-               q_out: Optional[torch.Tensor] = None, k_out: Optional[torch.Tensor] = None, inverse: bool = False, stream=None) -> None:
-    """Turn q [batch, n_q_heads, rows, head_dim] and k [batch, n_kv_heads, rows, head_dim] (either may be None) by
-    ``positions`` ([rows] or [batch, rows], int64).  Outputs default to their inputs (in place)."""
+
+def _rotary_plan(q, k, positions, q_out, k_out, inverse):
     x = q if q is not None else k
     _refuse(x is None, "q and k are both None")
     _refuse(x.dim() != 4, "q and k have four dimensions")
-    _refuse(rope.scaling not in _SCALING, "unknown scaling %r", rope.scaling)
     b, _, rows, d = x.shape
     code = _dtype(x, "q or k")
     _refuse(q is None and q_out is not None or k is None and k_out is not None, "an output without its input")
-    q_out = q if q_out is None else q_out
-    k_out = k if k_out is None else k_out
     for t, o, name in ((q, q_out, "q"), (k, k_out, "k")):
         if t is not None:
             _rows4(t, name, b, None, rows, d, x.dtype)
@@ -154,17 +192,27 @@ def kvc_rotary(rope: Rotary, q: Optional[torch.Tensor], k: Optional[torch.Tensor
     _refuse(tuple(positions.shape) not in ((rows,), (b, rows), (1, rows)), "positions has shape %s, not [%d] or [%d, %d]",
             tuple(positions.shape), rows, b, rows)
     _refuse(rows > 1 and positions.stride(-1) != 1, "a sequence's positions must be contiguous")
-    _one_device(x, k, positions, q_out, k_out)
-    desc = KvcRopeDesc(b, q.shape[1] if q is not None else 0, k.shape[1] if k is not None else 0, d, rows, rope.rot_dim, code,
-                       int(rope.interleaved), int(inverse), _SCALING[rope.scaling], rope.theta, rope.factor, rope.turns_low,
-                       rope.turns_high, rope.original_ctx, rope.mscale)
+    desc = KvcRopeDesc(b, q.shape[1] if q is not None else 0, k.shape[1] if k is not None else 0, d, rows, code, int(inverse), 0)
     if q is not None:
         desc.q_stride, desc.q_out_stride = _strides(q), _strides(q_out)
     if k is not None:
         desc.k_stride, desc.k_out_stride = _strides(k), _strides(k_out)
     per_sequence = positions.stride(0) if positions.dim() == 2 and positions.shape[0] > 1 else 0
-    _check(_load().kvc_rotary(C.byref(desc), _dptr(q), _dptr(k), _dptr(positions), per_sequence, _dptr(q_out), _dptr(k_out),
-                              _stream(stream)))
+    return C.byref(desc), per_sequence, _one_device(x, k, positions, q_out, k_out)
+
+
+def kvc_rotary(rope: Rotary, q: Optional[torch.Tensor], k: Optional[torch.Tensor], positions: torch.Tensor,
+               q_out: Optional[torch.Tensor] = None, k_out: Optional[torch.Tensor] = None, inverse: bool = False, stream=None) -> None:
+    """Turn q [batch, n_q_heads, rows, head_dim] and k [batch, n_kv_heads, rows, head_dim] (either may be None) by
+    ``positions`` ([rows] or [batch, rows], int64).  Outputs default to their inputs (in place)."""
+    if q_out is None:
+        q_out = q
+    if k_out is None:
+        k_out = k
+    key = (_sig(q), _sig(k), _sig(positions), _sig(q_out), _sig(k_out), inverse)
+    plan = rope.plans.get(key) or rope.plans.keep(key, _rotary_plan(q, k, positions, q_out, k_out, inverse))
+    _check(_load().kvc_rotary(rope.ref, plan[0], _ptr(q), _ptr(k), positions.data_ptr(), plan[1], _ptr(q_out), _ptr(k_out),
+                              _launch_stream(plan[2], stream)))
 
 
 def kvc_cache_gather(desc, k: Sequence[torch.Tensor], v: Sequence[torch.Tensor], idx: Optional[torch.Tensor],
@@ -175,24 +223,24 @@ def kvc_cache_gather(desc, k: Sequence[torch.Tensor], v: Sequence[torch.Tensor],
     L, b, h, n = desc.n_layers, desc.batch, desc.n_kv_heads, desc.n_ctx
     _refuse(not (len(k) == len(v) == len(caches) == L), "k, v and caches hold one entry per layer (%d)", L)
     dtype = torch.float32 if desc.dtype == F32 else torch.bfloat16
-    for t in (*k, *v):
-        _rows4(t, "k or v", b, h, n, desc.head_dim, dtype)
+    _rows4(k[0], "k or v", b, h, n, desc.head_dim, dtype)
     given = list(desc.kv_stride) if desc.kv_stride[0] else [h * n * desc.head_dim, n * desc.head_dim, desc.head_dim]
+    _refuse(any(k[0].shape[i] > 1 and k[0].stride(i) != given[i] for i in range(3)), "k or v has other strides than desc.kv_stride")
+    like = _sig(k[0])
     for t in (*k, *v):
-        _refuse(any(t.shape[i] > 1 and t.stride(i) != given[i] for i in range(3)), "k or v has other strides than desc.kv_stride")
+        if _sig(t) != like:             # (another stride of a dimension of one is none)
+            _rows4(t, "k or v", b, h, n, desc.head_dim, dtype)
+            _refuse(any(t.shape[i] > 1 and t.stride(i) != given[i] for i in range(3)), "k or v has other strides than desc.kv_stride")
     _dense(idx, "idx", torch.int32, L, b, h, n)
     _dense(n_keep, "n_keep", torch.int32, *((b, L, h) if per_head else (b, L)))
     _refuse(device_status is not None and device_status.dtype != torch.int32, "device_status must be int32")
-    _one_device(k[0], *k, *v, idx, n_keep, device_status, *(c.k for c in caches))
+    dev = _one_device(k[0], *k, *v, idx, n_keep, device_status, *(c.k for c in caches))
     structs = (KvcCache * L)(*(c.struct for c in caches))
-    _check(_load().kvc_cache_gather(C.byref(desc), _ptr_array(k), _ptr_array(v), _dptr(idx), _dptr(n_keep), int(per_head), structs,
-                                    _dptr(device_status), _stream(stream)))
+    _check(_load().kvc_cache_gather(C.byref(desc), _ptr_array(k), _ptr_array(v), _ptr(idx), _ptr(n_keep), int(per_head), structs,
+                                    _ptr(device_status), _launch_stream(dev, stream)))
 
 
-def kvc_cache_append(cache: Cache, k_new: torch.Tensor, v_new: torch.Tensor, n_new: Optional[torch.Tensor] = None,
-                     lengths_out: Optional[torch.Tensor] = None, weight: Optional[torch.Tensor] = None,
-                     device_status: Optional[torch.Tensor] = None, stream=None) -> None:
-    """Rows of new tokens [batch, Hkv, rows, head_dim] behind the ones in use; ``n_new`` [batch] int32 of them per sequence."""
+def _append_plan(cache, k_new, v_new, n_new, lengths_out, weight, device_status):
     b, h = cache.batch, cache.n_kv_heads
     code = _dtype(k_new, "k_new")
     _rows4(k_new, "k_new", b, h, None, cache.head_dim)
@@ -203,14 +251,20 @@ def kvc_cache_append(cache: Cache, k_new: torch.Tensor, v_new: torch.Tensor, n_n
     _dense(lengths_out, "lengths_out", torch.int32, b, h)
     _dense(weight, "weight", torch.float32, b, h, cache.capacity)
     _refuse(device_status is not None and device_status.dtype != torch.int32, "device_status must be int32")
-    _one_device(cache.k, k_new, v_new, n_new, lengths_out, weight, device_status)
-    _check(_load().kvc_cache_append(C.byref(cache.struct), _dptr(k_new), _dptr(v_new), code, k_new.shape[2], strides, _dptr(n_new),
-                                    _dptr(lengths_out), _dptr(weight), _dptr(device_status), _stream(stream)))
+    return code, k_new.shape[2], strides, _one_device(cache.k, k_new, v_new, n_new, lengths_out, weight, device_status)
 
 
-def kvc_cache_read(cache: Cache, k_out: Optional[torch.Tensor], v_out: Optional[torch.Tensor], first: Optional[torch.Tensor] = None,
-                   stream=None) -> None:
-    """Values of the rows first[b, h] .. into k_out, v_out [batch, Hkv, rows, head_dim] (bf16 or fp32, contiguous)."""
+def kvc_cache_append(cache: Cache, k_new: torch.Tensor, v_new: torch.Tensor, n_new: Optional[torch.Tensor] = None,
+                     lengths_out: Optional[torch.Tensor] = None, weight: Optional[torch.Tensor] = None,
+                     device_status: Optional[torch.Tensor] = None, stream=None) -> None:
+    """Rows of new tokens [batch, Hkv, rows, head_dim] behind the ones in use; ``n_new`` [batch] int32 of them per sequence."""
+    key = ("append", _sig(k_new), _sig(v_new), _sig(n_new), _sig(lengths_out), _sig(weight), _sig(device_status))
+    plan = cache.plans.get(key) or cache.plans.keep(key, _append_plan(cache, k_new, v_new, n_new, lengths_out, weight, device_status))
+    _check(_load().kvc_cache_append(cache.ref, k_new.data_ptr(), v_new.data_ptr(), plan[0], plan[1], plan[2], _ptr(n_new), _ptr(lengths_out),
+                                    _ptr(weight), _ptr(device_status), _launch_stream(plan[3], stream)))
+
+
+def _read_plan(cache, k_out, v_out, first):
     x = k_out if k_out is not None else v_out
     _refuse(x is None, "k_out and v_out are both None")
     code = _dtype(x, "k_out or v_out")
@@ -218,8 +272,15 @@ def kvc_cache_read(cache: Cache, k_out: Optional[torch.Tensor], v_out: Optional[
     for t in (k_out, v_out):
         _dense(t, "k_out or v_out", x.dtype, cache.batch, cache.n_kv_heads, x.shape[2], cache.head_dim)
     _dense(first, "first", torch.int32, cache.batch, cache.n_kv_heads)
-    _one_device(cache.k, k_out, v_out, first)
-    _check(_load().kvc_cache_read(C.byref(cache.struct), _dptr(first), x.shape[2], code, _dptr(k_out), _dptr(v_out), _stream(stream)))
+    return code, x.shape[2], _one_device(cache.k, k_out, v_out, first)
+
+
+def kvc_cache_read(cache: Cache, k_out: Optional[torch.Tensor], v_out: Optional[torch.Tensor], first: Optional[torch.Tensor] = None,
+                   stream=None) -> None:
+    """Values of the rows first[b, h] .. into k_out, v_out [batch, Hkv, rows, head_dim] (bf16 or fp32, contiguous)."""
+    key = ("read", _sig(k_out), _sig(v_out), _sig(first))
+    plan = cache.plans.get(key) or cache.plans.keep(key, _read_plan(cache, k_out, v_out, first))
+    _check(_load().kvc_cache_read(cache.ref, _ptr(first), plan[1], plan[0], _ptr(k_out), _ptr(v_out), _launch_stream(plan[2], stream)))
 
 
 def _attend_desc(cache: Cache, q: torch.Tensor, out: Optional[torch.Tensor], causal: bool, scale: float) -> KvcAttendDesc:
@@ -236,8 +297,19 @@ def kvc_attend_workspace_size(cache: Cache, q: torch.Tensor, with_weight: bool) 
     """Bytes of scratch ``kvc_attend`` needs for queries of q's shape; with_weight: with the tokens' weights."""
     out = C.c_size_t(0)
     desc = _attend_desc(cache, q, None, True, 0.0)
-    _check(_load().kvc_attend_workspace_size(C.byref(cache.struct), C.byref(desc), int(with_weight), C.byref(out)))
+    _check(_load().kvc_attend_workspace_size(cache.ref, C.byref(desc), int(with_weight), C.byref(out)))
     return int(out.value)
+
+
+def _attend_plan(cache, q, out, lse, weight, weight_out, row_counts, causal, scale, workspace):
+    b, h = cache.batch, cache.n_kv_heads
+    desc = _attend_desc(cache, q, out, causal, scale)
+    _dense(lse, "lse", torch.float32, b, q.shape[1], q.shape[2])
+    _dense(weight, "weight", torch.float32, b, h, cache.capacity)
+    _dense(weight_out, "weight_out", torch.float32, b, h, cache.capacity)
+    _dense(row_counts, "row_counts", torch.int32, b)
+    dev = _one_device(cache.k, q, out, lse, weight, weight_out, row_counts, workspace)
+    return C.byref(desc), 0 if workspace is None else workspace.numel() * workspace.element_size(), dev
 
 
 def kvc_attend(cache: Cache, q: torch.Tensor, out: torch.Tensor, lse: Optional[torch.Tensor] = None,
@@ -246,28 +318,28 @@ def kvc_attend(cache: Cache, q: torch.Tensor, out: torch.Tensor, lse: Optional[t
                workspace: Optional[torch.Tensor] = None, stream=None) -> None:
     """Attention of q [batch, n_q_heads, rows, head_dim] over the cache into out.  lse [batch, n_q_heads, rows] fp32.
     weight [batch, Hkv, capacity] fp32: the tokens' running weight, added to in place, or into ``weight_out``."""
-    desc = _attend_desc(cache, q, out, causal, scale)
-    b, h = cache.batch, cache.n_kv_heads
     if weight_out is None:
         weight_out = weight
-    _dense(lse, "lse", torch.float32, b, q.shape[1], q.shape[2])
-    _dense(weight, "weight", torch.float32, b, h, cache.capacity)
-    _dense(weight_out, "weight_out", torch.float32, b, h, cache.capacity)
-    _dense(row_counts, "row_counts", torch.int32, b)
-    _one_device(cache.k, q, out, lse, weight, weight_out, row_counts, workspace)
-    wp, wb = _ws(workspace)
-    _check(_load().kvc_attend(C.byref(cache.struct), C.byref(desc), _dptr(q), _dptr(row_counts), _dptr(out), _dptr(lse), _dptr(weight),
-                              _dptr(weight_out), wp, wb, _stream(stream)))
+    key = ("attend", _sig(q), _sig(out), _sig(lse), _sig(weight), _sig(weight_out), _sig(row_counts), causal, scale, _sig(workspace))
+    plan = cache.plans.get(key) or cache.plans.keep(
+        key, _attend_plan(cache, q, out, lse, weight, weight_out, row_counts, causal, scale, workspace))
+    _check(_load().kvc_attend(cache.ref, plan[0], q.data_ptr(), _ptr(row_counts), out.data_ptr(), _ptr(lse), _ptr(weight), _ptr(weight_out),
+                              _ptr(workspace), plan[1], _launch_stream(plan[2], stream)))
+
+
+def _evict_plan(src, dst, weight, budget, idx_out, weight_out):
+    b, h = src.batch, src.n_kv_heads
+    _dense(weight, "weight", torch.float32, b, h, src.capacity)
+    _dense(idx_out, "idx_out", torch.int32, b, h, int(budget))
+    _dense(weight_out, "weight_out", torch.float32, b, h, dst.capacity)
+    return (_one_device(src.k, dst.k, weight, idx_out, weight_out),)
 
 
 def kvc_evict(src: Cache, dst: Cache, weight: torch.Tensor, budget: int, recent: int, idx_out: torch.Tensor,
               weight_out: Optional[torch.Tensor] = None, stream=None) -> None:
     """The last ``recent`` rows of every head and the heaviest of the others, ``budget`` in all, from src into dst; their
     positions go to idx_out [batch, Hkv, budget] int32, their weights to weight_out [batch, Hkv, dst.capacity]."""
-    b, h = src.batch, src.n_kv_heads
-    _dense(weight, "weight", torch.float32, b, h, src.capacity)
-    _dense(idx_out, "idx_out", torch.int32, b, h, int(budget))
-    _dense(weight_out, "weight_out", torch.float32, b, h, dst.capacity)
-    _one_device(src.k, dst.k, weight, idx_out, weight_out)
-    _check(_load().kvc_evict(C.byref(src.struct), C.byref(dst.struct), _dptr(weight), int(budget), int(recent), _dptr(idx_out),
-                             _dptr(weight_out), _stream(stream)))
+    key = ("evict", dst.capacity, dst.k.get_device(), _sig(weight), budget, _sig(idx_out), _sig(weight_out))
+    plan = src.plans.get(key) or src.plans.keep(key, _evict_plan(src, dst, weight, budget, idx_out, weight_out))
+    _check(_load().kvc_evict(src.ref, dst.ref, weight.data_ptr(), int(budget), int(recent), idx_out.data_ptr(), _ptr(weight_out),
+                             _launch_stream(plan[0], stream)))
