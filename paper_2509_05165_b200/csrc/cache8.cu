@@ -2,8 +2,8 @@
 // (kvc_cache_read).
 //
 // The unit of work is a block of tokens of one head, K or V: its exponent needs the largest of its block * d values before
-// the first code can be rounded, so a job of block * d / 32 threads holds the block in registers, 32 values per thread,
-// reduces the maximum once and writes codes.  Every source row is read once and every code written once; HBM is the bound.
+// the first code can be rounded, so a job of block * d / 32 threads holds a block of K and the one of V beside it in registers,
+// 32 values of each per thread (as loaded: maxima are taken over the bits), reduces both maxima at once and writes codes.  Every source row is read once and every code written once; HBM is the bound.
 #include "cache8.cuh"
 
 namespace kvc {
@@ -29,30 +29,28 @@ template <typename T, int kFormat>
 __global__ void __launch_bounds__(512)
 cache_gather_kernel(const __grid_constant__ CacheGatherParams P, const int32_t* __restrict__ idx,
                     const int32_t* __restrict__ n_keep, int32_t* device_status) {
-  __shared__ float scratch[16];
+  __shared__ float2 scratch[16];
   grid_dependency_wait();
-  const int l = blockIdx.z >> 1, is_v = blockIdx.z & 1;
-  const int unit = blockIdx.y, b = unit / P.Hkv, h = unit - b * P.Hkv;
+  const int l = blockIdx.z, unit = blockIdx.y, b = unit / P.Hkv, h = unit - b * P.Hkv;
   const GatherLayer& y = P.layer[l];
   long long n = P.N;
   if (n_keep != nullptr) {
     n = P.per_head ? n_keep[((long long)b * P.L + l) * P.Hkv + h] : n_keep[(long long)b * P.L + l];
     n = n < 0 ? 0 : (n > P.N ? P.N : n);
   }
-  if (blockIdx.x == 0 && is_v == 0 && threadIdx.x == 0) {
+  if (blockIdx.x == 0 && threadIdx.x == 0) {
     y.lengths[unit] = (int32_t)(n < y.cap ? n : y.cap);
     if (n > y.cap && device_status != nullptr) *device_status = KVC_ERR_CAPACITY;
   }
   if (n > y.cap) n = y.cap;
 
-  const JobLane j(P.block_shift, P.d);
-  const long long blk = (long long)blockIdx.x * (blockDim.x / j.threads) + j.slot;
-  const long long row0 = blk << P.block_shift;
-  if (((long long)blockIdx.x * (blockDim.x / j.threads) << P.block_shift) >= n) return;    // (the whole CTA)
-  const T* src = reinterpret_cast<const T*>(is_v ? y.v : y.k) + b * P.kvs[0] + h * P.kvs[1];
+  const JobLane<8> j(P.block_shift, P.d);
+  const int slots = blockDim.x / j.threads;
+  if (((long long)blockIdx.x * slots << P.block_shift) >= n) return;    // (the whole CTA)
+  const long long blk = (long long)blockIdx.x * slots + j.slot, row0 = blk << P.block_shift;
+  const long long from = b * P.kvs[0] + h * P.kvs[1];
+  const T *ks = reinterpret_cast<const T*>(y.k) + from, *vs = reinterpret_cast<const T*>(y.v) + from;
   const int32_t* map = idx == nullptr ? nullptr : idx + (((long long)l * P.Bt + b) * P.Hkv + h) * P.N;
-  float x[4][8];
-  float top = 0.f;
   long long at[4];
 #pragma unroll
   for (int g = 0; g < 4; ++g) {
@@ -63,38 +61,46 @@ cache_gather_kernel(const __grid_constant__ CacheGatherParams P, const int32_t* 
       if (at[g] >= P.N) at[g] = -1;
     }
   }
+  Raw8<T> kx[4], vx[4];
 #pragma unroll
   for (int g = 0; g < 4; ++g) {
     if (at[g] >= 0) {
-      load8<T>(src + at[g] * P.kvs[2] + j.col(g), x[g]);
+      kx[g].load(ks + at[g] * P.kvs[2] + j.col(g));
+      vx[g].load(vs + at[g] * P.kvs[2] + j.col(g));
     } else {
-#pragma unroll
-      for (int i = 0; i < 8; ++i) x[g][i] = 0.f;
+      kx[g].zero();
+      vx[g].zero();
     }
   }
-#pragma unroll
-  for (int g = 0; g < 4; ++g)
-#pragma unroll
-    for (int i = 0; i < 8; ++i) top = fmaxf(top, fabsf(x[g][i]));
-  const int e = exponent_of<kFormat>(job_max(top, j, scratch));
-  if (row0 >= n) return;
-  const float f = pow2(-e);
-  uint8_t* out = (is_v ? y.vo : y.ko) + b * y.st[0] + h * y.st[1];
+  uint32_t km = 0, vm = 0;
 #pragma unroll
   for (int g = 0; g < 4; ++g) {
-    const long long r = row0 + j.row(g);
-    if (r < n)
-      *reinterpret_cast<uint2*>(out + r * y.st[2] + j.col(g)) =
-          make_uint2(encode4<kFormat>(x[g][0], x[g][1], x[g][2], x[g][3], f), encode4<kFormat>(x[g][4], x[g][5], x[g][6], x[g][7], f));
+    km = kx[g].max_bits(km);
+    vm = vx[g].max_bits(vm);
   }
-  if (j.t == 0) (is_v ? y.ve : y.ke)[(long long)unit * y.blocks + blk] = (int8_t)e;
+  const float2 top = job_max(make_float2(Raw8<T>::top(km), Raw8<T>::top(vm)), j, scratch);
+  if (row0 >= n) return;
+  const int ke = exponent_of<kFormat>(top.x), ve = exponent_of<kFormat>(top.y);
+  const long long to = b * y.st[0] + h * y.st[1];
+#pragma unroll
+  for (int g = 0; g < 4; ++g) {
+    const long long r = row0 + j.row(g), o = to + r * y.st[2] + j.col(g);
+    if (r < n) {
+      *reinterpret_cast<uint2*>(y.ko + o) = kx[g].template encode<kFormat>(pow2(-ke));
+      *reinterpret_cast<uint2*>(y.vo + o) = vx[g].template encode<kFormat>(pow2(-ve));
+    }
+  }
+  if (j.t == 0) {
+    y.ke[(long long)unit * y.blocks + blk] = (int8_t)ke;
+    y.ve[(long long)unit * y.blocks + blk] = (int8_t)ve;
+  }
 }
 
 // ---- new tokens -------------------------------------------------------------------------------------------------------
 
 struct AppendParams {
   Cache c;
-  int rows, jobs_per_cta;                // jobs_per_cta: blocks (of K and of V) that a CTA takes, per grid step
+  int rows, jobs_per_cta;                // jobs_per_cta: blocks (of K and V) that a CTA takes
   long long ns[3];
   bool write_lengths;                    // the lengths are written here (else by append_lengths_kernel)
 };
@@ -104,84 +110,94 @@ __device__ __forceinline__ int rows_of(const AppendParams& P, const int32_t* n_n
   return n < 0 ? 0 : (n > P.rows ? P.rows : n);
 }
 
+// Eight codes in place, rounded again for an exponent larger by -down.
+template <int kFormat>
+__device__ __forceinline__ void regrow(uint8_t* p, int down) {
+  const uint2 w = *reinterpret_cast<const uint2*>(p);
+  const float f = pow2_clamped(down);
+  float y[8];
+  decode4<kFormat>(w.x, y);
+  decode4<kFormat>(w.y, y + 4);
+  *reinterpret_cast<uint2*>(p) = make_uint2(encode4<kFormat>(y[0], y[1], y[2], y[3], f), encode4<kFormat>(y[4], y[5], y[6], y[7], f));
+}
+
 // A CTA takes blocks blockIdx.x * jobs_per_cta .. of the ones that a head's new rows touch, counted from its open block.
 template <typename T, int kFormat>
 __global__ void __launch_bounds__(512)
 cache_append_kernel(const __grid_constant__ AppendParams P, const T* __restrict__ k_new, const T* __restrict__ v_new,
                     const int32_t* __restrict__ n_new, int32_t* lengths_out, float* __restrict__ weight, int32_t* device_status) {
-  __shared__ float scratch[16];
+  __shared__ float2 scratch[16];
   grid_dependency_wait();
   const Cache& c = P.c;
   const int unit = blockIdx.y, b = unit / c.Hkv, h = unit - b * c.Hkv;
-  const long long len = c.length(unit);
+  const int len = (int)c.length(unit);
   const int want = rows_of(P, n_new, b);
-  const int n = (int)(want < c.cap - len ? want : c.cap - len);
+  const int n = (int)min((long long)want, c.cap - len);
   __syncthreads();                       // every thread has the length before it may change
   if (blockIdx.x == 0 && threadIdx.x == 0) {
-    if (P.write_lengths) lengths_out[unit] = (int32_t)(len + n);
+    if (P.write_lengths) lengths_out[unit] = len + n;
     if (n < want && device_status != nullptr) *device_status = KVC_ERR_CAPACITY;
   }
   if (n == 0) return;
-  const JobLane j(c.block_shift, c.d);
+  const JobLane<8> j(c.block_shift, c.d);
   const int slots = blockDim.x / j.threads;
-  const long long blk0 = len >> c.block_shift;
-  const int touched = (int)(((len + n - 1) >> c.block_shift) - blk0) + 1;
-  const int first = blockIdx.x * P.jobs_per_cta, last = min(first + P.jobs_per_cta, touched);
-  // jobs: block `first`'s K and V, the next block's, ...
-  for (int jb = 2 * first; jb < 2 * last; jb += slots) {
-    const int job = jb + j.slot;
-    const bool live = job < 2 * last;
-    const int is_v = job & 1;
-    const long long blk = blk0 + (job >> 1), row0 = blk << c.block_shift;
-    uint8_t* codes = (is_v ? c.v : c.k) + c.base(unit);
-    int8_t* exps = (is_v ? c.v_exp : c.k_exp) + (long long)unit * c.blocks;
-    const T* src = (is_v ? v_new : k_new) + b * P.ns[0] + h * P.ns[1];
-    float x[4][8];
-    float top = 0.f;
+  const int blk0 = len >> c.block_shift, touched = ((len + n - 1) >> c.block_shift) - blk0 + 1;
+  const int last = min((int)(blockIdx.x + 1) * P.jobs_per_cta, touched);
+  const long long from = b * P.ns[0] + h * P.ns[1];
+  for (int jb = blockIdx.x * P.jobs_per_cta; jb < last; jb += slots) {
+    const bool live = jb + j.slot < last;
+    const int blk = blk0 + jb + j.slot, row0 = blk << c.block_shift;
+    Raw8<T> kx[4], vx[4];
+    uint32_t km = 0, vm = 0;
 #pragma unroll
     for (int g = 0; g < 4; ++g) {
-      const long long r = row0 + j.row(g) - len;          // the row's number among the new ones
+      const int r = row0 + j.row(g) - len;                // the row's number among the new ones
       if (live && r >= 0 && r < n) {
-        load8<T>(src + r * P.ns[2] + j.col(g), x[g]);
-        if (weight != nullptr && is_v == 0 && j.col(g) == 0) weight[unit * c.cap + len + r] = 0.f;
+        const long long at = from + r * P.ns[2] + j.col(g);
+        kx[g].load(k_new + at);
+        vx[g].load(v_new + at);
+        if (weight != nullptr && j.col(g) == 0) weight[unit * c.cap + len + r] = 0.f;
       } else {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) x[g][i] = 0.f;
-      }
-#pragma unroll
-      for (int i = 0; i < 8; ++i) top = fmaxf(top, fabsf(x[g][i]));
-    }
-    int e = exponent_of<kFormat>(job_max(top, j, scratch));
-    if (!live) continue;
-    if (row0 < len) {                                     // the open block has rows already
-      const int was = exps[blk];
-      e = max(e, was);
-      if (e > was) {
-        const float f = pow2_clamped(was - e);
-#pragma unroll
-        for (int g = 0; g < 4; ++g) {
-          if (row0 + j.row(g) < len) {
-            uint2* p = reinterpret_cast<uint2*>(codes + (row0 + j.row(g)) * c.st[2] + j.col(g));
-            const uint2 w = *p;
-            float y[8];
-            decode4<kFormat>(w.x, y);
-            decode4<kFormat>(w.y, y + 4);
-            *p = make_uint2(encode4<kFormat>(y[0], y[1], y[2], y[3], f), encode4<kFormat>(y[4], y[5], y[6], y[7], f));
-          }
-        }
+        kx[g].zero();
+        vx[g].zero();
       }
     }
-    const float f = pow2(-e);
 #pragma unroll
     for (int g = 0; g < 4; ++g) {
-      const long long r = row0 + j.row(g);
-      if (r >= len && r < len + n)
-        *reinterpret_cast<uint2*>(codes + r * c.st[2] + j.col(g)) =
-            make_uint2(encode4<kFormat>(x[g][0], x[g][1], x[g][2], x[g][3], f), encode4<kFormat>(x[g][4], x[g][5], x[g][6], x[g][7], f));
+      km = kx[g].max_bits(km);
+      vm = vx[g].max_bits(vm);
     }
-    // every thread of the job has read the old exponent before it changes
+    const float2 top = job_max(make_float2(Raw8<T>::top(km), Raw8<T>::top(vm)), j, scratch);
+    if (!live) continue;
+    const long long eat = (long long)unit * c.blocks + blk;
+    int ke = exponent_of<kFormat>(top.x), ve = exponent_of<kFormat>(top.y);
+    const bool open = row0 < len;                         // the block has rows already
+    int kwas = kExpMin, vwas = kExpMin;
+    if (open) {
+      kwas = c.k_exp[eat];
+      vwas = c.v_exp[eat];
+      ke = max(ke, kwas);
+      ve = max(ve, vwas);
+    }
+    const long long to = c.base(unit);
+#pragma unroll
+    for (int g = 0; g < 4; ++g) {
+      const int r = row0 + j.row(g);
+      const long long o = to + r * c.st[2] + j.col(g);
+      if (r >= len && r < len + n) {
+        *reinterpret_cast<uint2*>(c.k + o) = kx[g].template encode<kFormat>(pow2(-ke));
+        *reinterpret_cast<uint2*>(c.v + o) = vx[g].template encode<kFormat>(pow2(-ve));
+      } else if (open && r < len && (ke > kwas || ve > vwas)) {      // a code under a larger exponent: rounded again
+        if (ke > kwas) regrow<kFormat>(c.k + o, kwas - ke);
+        if (ve > vwas) regrow<kFormat>(c.v + o, vwas - ve);
+      }
+    }
+    // every thread of the job has read the old exponents before they change
     if (j.threads == 32) __syncwarp(); else asm volatile("bar.sync %0, %1;" :: "r"(1 + j.slot), "r"(j.threads) : "memory");
-    if (j.t == 0) exps[blk] = (int8_t)e;
+    if (j.t == 0) {
+      c.k_exp[eat] = (int8_t)ke;
+      c.v_exp[eat] = (int8_t)ve;
+    }
   }
 }
 
@@ -247,7 +263,7 @@ kvc_status run_gather(const CacheGatherParams& P, int format, int block, long lo
                       int32_t* status, cudaStream_t st) {
   const int job = block * P.d / 32, threads = job > 256 ? job : 256;
   const long long rows = most_cap < P.N ? most_cap : P.N, per_cta = (long long)(threads / job) * block;
-  const dim3 grid((unsigned)((rows + per_cta - 1) / per_cta), P.Bt * P.Hkv, 2 * P.L);
+  const dim3 grid((unsigned)((rows + per_cta - 1) / per_cta), P.Bt * P.Hkv, P.L);
   auto kernel = format == KVC_E4M3 ? cache_gather_kernel<T, KVC_E4M3> : cache_gather_kernel<T, KVC_INT8>;
   KVC_CUDA(launch_dependent(kernel, grid, dim3(threads), 0, st, P, idx, n_keep, status));
   KVC_LAUNCH_CHECK("cache_gather_kernel");

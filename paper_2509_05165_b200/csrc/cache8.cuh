@@ -99,49 +99,125 @@ __device__ __forceinline__ uint4 ld16_stream(const void* p) {
   return v;
 }
 
-// A block's tokens as one job of block * d / 32 threads with 32 values each, four groups of eight: kFirst .. of a row.
+// The largest magnitude among 8-bit codes, as fp32.  pairs: two 16-bit maxima, of e4m3 magnitudes (as codes, whose order is
+// that of the values) or of int8 magnitudes.
+template <int kFormat>
+__device__ __forceinline__ uint32_t max_codes(uint32_t pairs, uint32_t w) {
+  if (kFormat == KVC_E4M3) return __vmaxu2(__vmaxu2(pairs, w & 0x007f007fu), (w >> 8) & 0x007f007fu);
+  uint32_t a, b;                          // sign-extended (a selector's fourth bit copies the byte's sign)
+  asm("prmt.b32 %0, %1, 0, 0x9180;" : "=r"(a) : "r"(w));
+  asm("prmt.b32 %0, %1, 0, 0xb3a2;" : "=r"(b) : "r"(w));
+  return __vmaxu2(__vmaxu2(pairs, __vabs2(a)), __vabs2(b));
+}
+template <int kFormat>
+__device__ __forceinline__ float max_value(uint32_t pairs) {
+  const uint32_t m = max(pairs & 0xffffu, pairs >> 16);
+  // (e4m3: the bits moved to fp32's place, whose exponents are biased by 120 more)
+  return kFormat == KVC_E4M3 ? __uint_as_float(m << 20) * pow2(120) : (float)m;
+}
+
+// A block's tokens as one job of block * d / 32 threads with 32 values of K and of V each, in groups of kGroup values of a row.
 // The jobs of a CTA lie side by side; a job is one warp or whole warps.
+template <int kGroup>
 struct JobLane {
-  int threads, slot, t, per_row_shift;    // per_row_shift: log2(d / 8)
+  static constexpr int kGroups = 32 / kGroup;
+  int threads, slot, t, per_row_shift;    // per_row_shift: log2(d / kGroup)
   __device__ __forceinline__ JobLane(int block_shift, int d) {
-    per_row_shift = d == 128 ? 4 : 3;
-    threads = 1 << (block_shift + per_row_shift - 2);
+    per_row_shift = (d == 128 ? 7 : 6) - (kGroup == 8 ? 3 : 4);
+    threads = 1 << (block_shift + (d == 128 ? 2 : 1));
     slot = threadIdx.x / threads;
     t = threadIdx.x - slot * threads;
   }
   __device__ __forceinline__ int row(int g) const { return (g * threads + t) >> per_row_shift; }
-  __device__ __forceinline__ int col(int g) const { return ((g * threads + t) & ((1 << per_row_shift) - 1)) * 8; }
+  __device__ __forceinline__ int col(int g) const { return ((g * threads + t) & ((1 << per_row_shift) - 1)) * kGroup; }
 };
 
-// The largest of a job's threads' values; every thread of the CTA calls it.  scratch: one float per warp.
-__device__ __forceinline__ float job_max(float x, const JobLane& j, float* scratch) {
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, o));
+// The largest of a job's threads' values (non-negative), of K and of V; every thread of the CTA calls it.  scratch: one per warp.
+template <typename Job>
+__device__ __forceinline__ float2 job_max(float2 x, const Job& j, float2* scratch) {
+  x.x = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(x.x)));
+  x.y = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(x.y)));
   if (j.threads == 32) return x;
   __syncthreads();                        // (the scratch of the call before has been read)
   if ((threadIdx.x & 31) == 0) scratch[threadIdx.x >> 5] = x;
   __syncthreads();
   const int w0 = j.slot * (j.threads >> 5);
   x = scratch[w0];
-  for (int i = 1; i < (j.threads >> 5); ++i) x = fmaxf(x, scratch[w0 + i]);
+  for (int i = 1; i < (j.threads >> 5); ++i) {
+    x.x = fmaxf(x.x, scratch[w0 + i].x);
+    x.y = fmaxf(x.y, scratch[w0 + i].y);
+  }
   return x;
+}
+
+// Eight values as they lie in memory.
+template <typename T>
+struct Raw8 {
+  uint4 w[sizeof(T) / 2];
+  __device__ __forceinline__ void load(const T* p) {          // (read once: past L1)
+#pragma unroll
+    for (int i = 0; i < (int)sizeof(T) / 2; ++i) w[i] = ld16_stream(reinterpret_cast<const char*>(p) + 16 * i);
+  }
+  __device__ __forceinline__ void load_coherent(const T* p) {
+#pragma unroll
+    for (int i = 0; i < (int)sizeof(T) / 2; ++i) w[i] = ld16(reinterpret_cast<const char*>(p) + 16 * i);
+  }
+  __device__ __forceinline__ void store(T* p) const {
+#pragma unroll
+    for (int i = 0; i < (int)sizeof(T) / 2; ++i) *reinterpret_cast<uint4*>(reinterpret_cast<char*>(p) + 16 * i) = w[i];
+  }
+  __device__ __forceinline__ void zero() {
+#pragma unroll
+    for (int i = 0; i < (int)sizeof(T) / 2; ++i) w[i] = make_uint4(0, 0, 0, 0);
+  }
+  __device__ __forceinline__ void values(float* x) const {
+    const uint32_t* u = &w[0].x;
+#pragma unroll
+    for (int i = 0; i < (int)sizeof(T) * 2; ++i) {
+      if (sizeof(T) == 2) {
+        x[2 * i] = __uint_as_float(u[i] << 16);
+        x[2 * i + 1] = __uint_as_float(u[i] & 0xffff0000u);
+      } else {
+        x[i] = __uint_as_float(u[i]);
+      }
+    }
+  }
+  // The magnitudes' bits, whose order is the values'; of bf16 two maxima side by side (see top()).
+  __device__ __forceinline__ uint32_t max_bits(uint32_t m) const {
+    const uint32_t* u = &w[0].x;
+#pragma unroll
+    for (int i = 0; i < (int)sizeof(T) * 2; ++i) m = sizeof(T) == 2 ? __vmaxu2(m, u[i] & 0x7fff7fffu) : max(m, u[i] & 0x7fffffffu);
+    return m;
+  }
+  static __device__ __forceinline__ float top(uint32_t m) {
+    return __uint_as_float(sizeof(T) == 2 ? max(m << 16, m & 0xffff0000u) : m);
+  }
+  template <int kFormat>
+  __device__ __forceinline__ uint2 encode(float f) const {
+    float x[8];
+    values(x);
+    return make_uint2(encode4<kFormat>(x[0], x[1], x[2], x[3], f), encode4<kFormat>(x[4], x[5], x[6], x[7], f));
+  }
+};
+
+// Sixteen codes rounded again after a change of exponent.
+template <int kFormat>
+__device__ __forceinline__ uint4 recode(uint4 w, float f) {
+  uint32_t* u = &w.x;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    float x[4];
+    decode4<kFormat>(u[i], x);
+    u[i] = encode4<kFormat>(x[0], x[1], x[2], x[3], f);
+  }
+  return w;
 }
 
 template <typename T>
 __device__ __forceinline__ void load8(const T* p, float* x) {
-  if (sizeof(T) == 2) {
-    const uint4 w = ld16_stream(p);
-    const uint32_t u[4] = {w.x, w.y, w.z, w.w};
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      x[2 * i] = __uint_as_float(u[i] << 16);
-      x[2 * i + 1] = __uint_as_float(u[i] & 0xffff0000u);
-    }
-  } else {
-    const uint4 a = ld16_stream(p), b = ld16_stream(p + 4);
-    x[0] = __uint_as_float(a.x); x[1] = __uint_as_float(a.y); x[2] = __uint_as_float(a.z); x[3] = __uint_as_float(a.w);
-    x[4] = __uint_as_float(b.x); x[5] = __uint_as_float(b.y); x[6] = __uint_as_float(b.z); x[7] = __uint_as_float(b.w);
-  }
+  Raw8<T> r;
+  r.load(p);
+  r.values(x);
 }
 
 // Threads of a CTA that works on blocks: at least 256, and whole jobs.

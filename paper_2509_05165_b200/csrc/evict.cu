@@ -123,59 +123,58 @@ evict_select_kernel(const __grid_constant__ EvictParams P, const float* __restri
 template <int kFormat>
 __global__ void __launch_bounds__(512)
 evict_move_kernel(const __grid_constant__ EvictParams P, const int32_t* __restrict__ idx_out) {
-  __shared__ float scratch[16];
+  __shared__ float2 scratch[16];
   grid_dependency_wait();
   const int unit = blockIdx.y;
-  const bool is_v = blockIdx.z == 1;
-  const long long n = P.dst.length(unit);
-  const JobLane j(P.dst.block_shift, P.dst.d);
-  const long long per_cta = (long long)(blockDim.x / j.threads) << P.dst.block_shift;
-  if (blockIdx.x * per_cta >= n) return;
-  const long long blk = (long long)blockIdx.x * (blockDim.x / j.threads) + j.slot, row0 = blk << P.dst.block_shift;
+  const int n = (int)P.dst.length(unit);
+  const JobLane<16> j(P.dst.block_shift, P.dst.d);
+  const int slots = blockDim.x / j.threads;
+  if (((long long)blockIdx.x * slots << P.dst.block_shift) >= n) return;
+  const int blk = blockIdx.x * slots + j.slot;
+  const long long row0 = (long long)blk << P.dst.block_shift;
   const int32_t* idx = idx_out + unit * P.budget;
-  const uint8_t* src = (is_v ? P.src.v : P.src.k) + P.src.base(unit);
-  const int8_t* exps = (is_v ? P.src.v_exp : P.src.k_exp) + (long long)unit * P.src.blocks;
-  uint8_t* out = (is_v ? P.dst.v : P.dst.k) + P.dst.base(unit);
-  uint2 w[4];
-  int es[4];
+  const uint8_t *ks = P.src.k + P.src.base(unit), *vs = P.src.v + P.src.base(unit);
+  const long long eb = (long long)unit * P.src.blocks;
+  int at[2];
 #pragma unroll
-  for (int g = 0; g < 4; ++g) {
-    const long long r = row0 + j.row(g);
-    w[g] = make_uint2(0, 0);
-    es[g] = kExpMin;
-    if (r < n) {
-      const long long at = idx[r];
-      w[g] = *reinterpret_cast<const uint2*>(src + at * P.src.st[2] + j.col(g));
-      es[g] = exps[at >> P.src.block_shift];
+  for (int g = 0; g < 2; ++g) at[g] = row0 + j.row(g) < n ? idx[row0 + j.row(g)] : -1;
+  uint4 kx[2], vx[2];
+  int ks_e[2], vs_e[2];
+#pragma unroll
+  for (int g = 0; g < 2; ++g) {
+    kx[g] = vx[g] = make_uint4(0, 0, 0, 0);
+    ks_e[g] = vs_e[g] = kExpMin;
+    if (at[g] >= 0) {
+      const long long o = at[g] * P.src.st[2] + j.col(g);
+      kx[g] = ld16_stream(ks + o);
+      vx[g] = ld16_stream(vs + o);
+      ks_e[g] = P.src.k_exp[eb + (at[g] >> P.src.block_shift)];
+      vs_e[g] = P.src.v_exp[eb + (at[g] >> P.src.block_shift)];
     }
   }
-  float top = 0.f;
+  float2 top = make_float2(0.f, 0.f);
 #pragma unroll
-  for (int g = 0; g < 4; ++g) {
-    float x[8], m = 0.f;
-    decode4<kFormat>(w[g].x, x);
-    decode4<kFormat>(w[g].y, x + 4);
-#pragma unroll
-    for (int i = 0; i < 8; ++i) m = fmaxf(m, fabsf(x[i]));
-    top = fmaxf(top, m * pow2_clamped(es[g]));
+  for (int g = 0; g < 2; ++g) {
+    const uint32_t km = max_codes<kFormat>(max_codes<kFormat>(max_codes<kFormat>(max_codes<kFormat>(0, kx[g].x), kx[g].y), kx[g].z), kx[g].w);
+    const uint32_t vm = max_codes<kFormat>(max_codes<kFormat>(max_codes<kFormat>(max_codes<kFormat>(0, vx[g].x), vx[g].y), vx[g].z), vx[g].w);
+    top.x = fmaxf(top.x, max_value<kFormat>(km) * pow2_clamped(ks_e[g]));
+    top.y = fmaxf(top.y, max_value<kFormat>(vm) * pow2_clamped(vs_e[g]));
   }
-  const int e = exponent_of<kFormat>(job_max(top, j, scratch));
+  top = job_max(top, j, scratch);
   if (row0 >= n) return;
+  const int ke = exponent_of<kFormat>(top.x), ve = exponent_of<kFormat>(top.y);
+  uint8_t *ko = P.dst.k + P.dst.base(unit), *vo = P.dst.v + P.dst.base(unit);
 #pragma unroll
-  for (int g = 0; g < 4; ++g) {
-    const long long r = row0 + j.row(g);
-    if (r >= n) continue;
-    uint2 y = w[g];
-    if (es[g] != e) {
-      float x[8];
-      decode4<kFormat>(w[g].x, x);
-      decode4<kFormat>(w[g].y, x + 4);
-      const float f = pow2_clamped(es[g] - e);
-      y = make_uint2(encode4<kFormat>(x[0], x[1], x[2], x[3], f), encode4<kFormat>(x[4], x[5], x[6], x[7], f));
-    }
-    *reinterpret_cast<uint2*>(out + r * P.dst.st[2] + j.col(g)) = y;
+  for (int g = 0; g < 2; ++g) {
+    if (at[g] < 0) continue;
+    const long long o = (row0 + j.row(g)) * P.dst.st[2] + j.col(g);
+    *reinterpret_cast<uint4*>(ko + o) = ks_e[g] == ke ? kx[g] : recode<kFormat>(kx[g], pow2_clamped(ks_e[g] - ke));
+    *reinterpret_cast<uint4*>(vo + o) = vs_e[g] == ve ? vx[g] : recode<kFormat>(vx[g], pow2_clamped(vs_e[g] - ve));
   }
-  if (j.t == 0) (is_v ? P.dst.v_exp : P.dst.k_exp)[(long long)unit * P.dst.blocks + blk] = (int8_t)e;
+  if (j.t == 0) {
+    P.dst.k_exp[(long long)unit * P.dst.blocks + blk] = (int8_t)ke;
+    P.dst.v_exp[(long long)unit * P.dst.blocks + blk] = (int8_t)ve;
+  }
 }
 
 bool overlap(const void* a, long long na, const void* b, long long nb) {
@@ -217,7 +216,7 @@ extern "C" kvc_status kvc_evict(const kvc_cache* src, const kvc_cache* dst, cons
   const int threads = job_cta_threads(b);
   const long long per_cta = (long long)(threads / (b.block * b.d / 32)) * b.block;
   KVC_CUDA(launch_dependent(b.format == KVC_E4M3 ? evict_move_kernel<KVC_E4M3> : evict_move_kernel<KVC_INT8>,
-                            dim3((unsigned)((budget + per_cta - 1) / per_cta), (unsigned)U, 2), dim3(threads), 0, st, P, idx_out));
+                            dim3((unsigned)((budget + per_cta - 1) / per_cta), (unsigned)U), dim3(threads), 0, st, P, idx_out));
   KVC_LAUNCH_CHECK("evict_move_kernel");
   return KVC_OK;
 }

@@ -1,8 +1,9 @@
 // Rotary positions (kvc_rotary): pair i of a row at position p is turned by the angle p f_i.
 //
-// Every value is read once and written once; the bound is HBM.  The angles of a row are the same in all of its heads, so
-// a CTA takes a tile of rows of one sequence with all heads (or, for few rows, a share of the heads), forms the tile's
-// cosines and sines in shared memory once, and streams the heads past them, 32 bytes of a row per thread and step.
+// Every value is read once and written once; the bound is HBM.  The angles of a row are the same in all of its heads, so a CTA
+// takes a tile of rows of one sequence with all heads (or, for few rows, a share of the heads), forms the tile's cosines and
+// sines in shared memory once, and each thread keeps its eight pairs of them in registers while it goes from head to head,
+// kRotUnroll heads' loads (32 bytes of a row each, 64 in fp32) in flight.
 // Angles: p f_i / 2pi in 64 bits, the whole turns taken off there (fp32 loses 0.008 rad at p = 131072, more than half a
 // step of bf16), the rest of a turn in fp32 through sincospif.
 #include <math.h>
@@ -14,9 +15,10 @@ namespace {
 
 constexpr int kRotThreads = 256;
 constexpr int kRotRows = 16;                 // rows of a tile
+constexpr int kRotUnroll = 4;                // heads in flight
 
 struct RotaryParams {
-  int Hq, Hkv, d, rows, rot, tile_rows, heads_per_cta;
+  int Hq, Hkv, d, rows, rot, tile_shift, heads_per_cta;      // tiles of 2^tile_shift rows
   long long qs[3], ks[3], qo[3], ko[3];
   long long pos_stride;
   float mscale;
@@ -40,22 +42,6 @@ __device__ __forceinline__ void store8(T* p, const float* x) {
   }
 }
 
-template <typename T>
-__device__ __forceinline__ void load8_any(const T* p, float* x) {   // (through the coherent path: an output may be its input)
-  if (sizeof(T) == 2) {
-    const uint4 w = ld16(p);
-    const uint32_t u[4] = {w.x, w.y, w.z, w.w};
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      x[2 * i] = __uint_as_float(u[i] << 16);
-      x[2 * i + 1] = __uint_as_float(u[i] & 0xffff0000u);
-    }
-  } else {
-    const float4 a = *reinterpret_cast<const float4*>(p), b = *reinterpret_cast<const float4*>(p + 4);
-    x[0] = a.x; x[1] = a.y; x[2] = a.z; x[3] = a.w; x[4] = b.x; x[5] = b.y; x[6] = b.z; x[7] = b.w;
-  }
-}
-
 // A step of a thread: 16 values of a row, eight pairs or, behind rot_dim, a copy.
 template <typename T, bool kInterleaved>
 __global__ void __launch_bounds__(kRotThreads)
@@ -63,8 +49,8 @@ rotary_kernel(const __grid_constant__ RotaryParams P, const T* q, const T* k, co
               T* k_out) {
   __shared__ float2 cs[kRotRows * 64];
   grid_dependency_wait();
-  const int row0 = blockIdx.x * P.tile_rows, b = blockIdx.y;
-  const int n = min(P.tile_rows, P.rows - row0), half = P.rot >> 1;
+  const int row0 = blockIdx.x << P.tile_shift, b = blockIdx.y;
+  const int n = min(1 << P.tile_shift, P.rows - row0), half = P.rot >> 1;
   for (int i = threadIdx.x; i < n * half; i += kRotThreads) {
     const int r = i / half, j = i - r * half;
     const double t = (double)positions[b * P.pos_stride + row0 + r] * P.turn[j];
@@ -74,44 +60,51 @@ rotary_kernel(const __grid_constant__ RotaryParams P, const T* q, const T* k, co
   }
   __syncthreads();
 
-  const int steps_shift = P.d == 128 ? 3 : 2;               // log2 of steps per row
-  const int per_head = n << steps_shift;
-  const int head0 = blockIdx.z * P.heads_per_cta;
-  const int heads = min(P.heads_per_cta, P.Hq + P.Hkv - head0);
-  for (int i = threadIdx.x; i < per_head * heads; i += kRotThreads) {
-    const int hh = i / per_head, rest = i - hh * per_head;
-    const int r = rest >> steps_shift, c = rest & ((1 << steps_shift) - 1);
-    int h = head0 + hh;
-    const T* in;
-    T* out;
-    if (h < P.Hq) {
-      in = q + b * P.qs[0] + h * P.qs[1] + (row0 + r) * P.qs[2];
-      out = q_out + b * P.qo[0] + h * P.qo[1] + (row0 + r) * P.qo[2];
-    } else {
-      h -= P.Hq;
-      in = k + b * P.ks[0] + h * P.ks[1] + (row0 + r) * P.ks[2];
-      out = k_out + b * P.ko[0] + h * P.ko[1] + (row0 + r) * P.ko[2];
-    }
-    float x[16], y[16];
-    if (16 * c >= P.rot) {
-      load8_any(in + 16 * c, x);
-      load8_any(in + 16 * c + 8, x + 8);
-      store8(out + 16 * c, x);
-      store8(out + 16 * c + 8, x + 8);
-      continue;
-    }
-    const int first = kInterleaved ? 16 * c : 8 * c, second = kInterleaved ? 16 * c + 8 : half + 8 * c;
-    load8_any(in + first, x);
-    load8_any(in + second, x + 8);
-    const float2* a = cs + r * half + 8 * c;
+  // thread: a step c of a row r, of every `side`-th head
+  const int steps_shift = P.d == 128 ? 3 : 2, shift = steps_shift + P.tile_shift, side = kRotThreads >> shift;
+  const int c = threadIdx.x & ((1 << steps_shift) - 1), r = (threadIdx.x & ((1 << shift) - 1)) >> steps_shift;
+  if (r >= n) return;
+  const bool copy = 16 * c >= P.rot;
+  const int first = copy || kInterleaved ? 16 * c : 8 * c, second = copy || kInterleaved ? 16 * c + 8 : half + 8 * c;
+  float2 a[8];
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      const int u = kInterleaved ? 2 * j : j, v = kInterleaved ? 2 * j + 1 : 8 + j;
-      y[u] = x[u] * a[j].x - x[v] * a[j].y;
-      y[v] = x[v] * a[j].x + x[u] * a[j].y;
+  for (int j = 0; j < 8; ++j) a[j] = copy ? make_float2(1.f, 0.f) : cs[r * half + 8 * c + j];
+  const long long row = row0 + r;
+  const T *qi = q + b * P.qs[0] + row * P.qs[2], *ki = k + b * P.ks[0] + row * P.ks[2];
+  T *qo = q_out + b * P.qo[0] + row * P.qo[2], *ko = k_out + b * P.ko[0] + row * P.ko[2];
+  const int head1 = min((int)(blockIdx.z + 1) * P.heads_per_cta, P.Hq + P.Hkv);
+  for (int h0 = blockIdx.z * P.heads_per_cta + (threadIdx.x >> shift); h0 < head1; h0 += side * kRotUnroll) {
+    Raw8<T> w[kRotUnroll][2];
+#pragma unroll
+    for (int u = 0; u < kRotUnroll; ++u) {
+      const int h = h0 + u * side;
+      if (h >= head1) break;
+      const T* in = h < P.Hq ? qi + h * P.qs[1] : ki + (h - P.Hq) * P.ks[1];
+      w[u][0].load_coherent(in + first);      // (an output may be its input)
+      w[u][1].load_coherent(in + second);
     }
-    store8(out + first, y);
-    store8(out + second, y + 8);
+#pragma unroll
+    for (int u = 0; u < kRotUnroll; ++u) {
+      const int h = h0 + u * side;
+      if (h >= head1) break;
+      T* out = h < P.Hq ? qo + h * P.qo[1] : ko + (h - P.Hq) * P.ko[1];
+      if (copy) {
+        w[u][0].store(out + first);
+        w[u][1].store(out + second);
+        continue;
+      }
+      float x[16], y[16];
+      w[u][0].values(x);
+      w[u][1].values(x + 8);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const int i0 = kInterleaved ? 2 * j : j, i1 = kInterleaved ? 2 * j + 1 : 8 + j;
+        y[i0] = x[i0] * a[j].x - x[i1] * a[j].y;
+        y[i1] = x[i1] * a[j].x + x[i0] * a[j].y;
+      }
+      store8(out + first, y);
+      store8(out + second, y + 8);
+    }
   }
 }
 
@@ -204,20 +197,22 @@ kvc_status kvc_rotary(const kvc_rope* R, const kvc_rope_desc* D, const void* q, 
   if (q && (s = resolve_strides(D->q_stride, D->batch, P.Hq, P.rows, P.d, eb, false, "q_stride", P.qs)) != KVC_OK) return s;
   if (q && (s = resolve_strides(D->q_out_stride, D->batch, P.Hq, P.rows, P.d, eb, true, "q_out_stride", P.qo)) != KVC_OK) return s;
   if (k && (s = resolve_strides(D->k_stride, D->batch, P.Hkv, P.rows, P.d, eb, false, "k_stride", P.ks)) != KVC_OK) return s;
+  if (!q) P.qs[0] = P.qs[1] = P.qs[2] = P.qo[0] = P.qo[1] = P.qo[2] = 0;
+  if (!k) P.ks[0] = P.ks[1] = P.ks[2] = P.ko[0] = P.ko[1] = P.ko[2] = 0;
   if (k && (s = resolve_strides(D->k_out_stride, D->batch, P.Hkv, P.rows, P.d, eb, true, "k_out_stride", P.ko)) != KVC_OK) return s;
   P.mscale = (float)R->mscale;
   if ((s = require_device()) != KVC_OK) return s;
   for (int i = 0; i < 64; ++i) P.turn[i] = D->inverse ? -R->turn[i] : R->turn[i];
 
-  P.tile_rows = P.rows < kRotRows ? P.rows : kRotRows;
-  const long long tiles = (P.rows + P.tile_rows - 1) / P.tile_rows;
+  P.tile_shift = 0;
+  while ((1 << P.tile_shift) < kRotRows && (1 << P.tile_shift) < P.rows) ++P.tile_shift;
+  const long long tiles = ((long long)P.rows + (1 << P.tile_shift) - 1) >> P.tile_shift;
   const int heads = P.Hq + P.Hkv;
   // few rows: a CTA takes only as many heads as give each of its threads a step
   P.heads_per_cta = heads;
   if (tiles * D->batch < 296) {
-    const int steps = P.tile_rows * P.d / 16;
-    P.heads_per_cta = (kRotThreads + steps - 1) / steps;
-    if (P.heads_per_cta > heads) P.heads_per_cta = heads;
+    const int steps = (P.d / 16) << P.tile_shift;
+    P.heads_per_cta = kRotThreads / steps < heads ? kRotThreads / steps : heads;
   }
   const dim3 grid((unsigned)tiles, D->batch, (heads + P.heads_per_cta - 1) / P.heads_per_cta);
   const bool il = R->interleaved != 0;
