@@ -211,6 +211,17 @@ __global__ void append_lengths_kernel(const __grid_constant__ AppendParams P, co
 
 // ---- values back ------------------------------------------------------------------------------------------------------
 
+// 32 bytes, a whole sector, at once (its address is a multiple of 16 at least).
+__device__ __forceinline__ void st32(void* p, const uint32_t* u) {
+  if ((reinterpret_cast<uintptr_t>(p) & 31u) == 0) {
+    asm volatile("st.global.v8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};"
+                 :: "l"(p), "r"(u[0]), "r"(u[1]), "r"(u[2]), "r"(u[3]), "r"(u[4]), "r"(u[5]), "r"(u[6]), "r"(u[7]) : "memory");
+  } else {
+    reinterpret_cast<uint4*>(p)[0] = make_uint4(u[0], u[1], u[2], u[3]);
+    reinterpret_cast<uint4*>(p)[1] = make_uint4(u[4], u[5], u[6], u[7]);
+  }
+}
+
 struct ReadParams {
   Cache c;
   long long rows;
@@ -248,12 +259,15 @@ cache_read_kernel(const __grid_constant__ ReadParams P, const int32_t* __restric
         const __nv_bfloat162 t = __floats2bfloat162_rn(x[2 * q] * f, x[2 * q + 1] * f);
         u[q] = *reinterpret_cast<const uint32_t*>(&t);
       }
-      reinterpret_cast<uint4*>(o)[0] = make_uint4(u[0], u[1], u[2], u[3]);
-      reinterpret_cast<uint4*>(o)[1] = make_uint4(u[4], u[5], u[6], u[7]);
+      st32(o, u);
     } else {
 #pragma unroll
-      for (int q = 0; q < 4; ++q)
-        reinterpret_cast<float4*>(o)[q] = make_float4(x[4 * q] * f, x[4 * q + 1] * f, x[4 * q + 2] * f, x[4 * q + 3] * f);
+      for (int h = 0; h < 2; ++h) {
+        uint32_t u[8];
+#pragma unroll
+        for (int q = 0; q < 8; ++q) u[q] = __float_as_uint(x[8 * h + q] * f);
+        st32(reinterpret_cast<char*>(o) + 32 * h, u);
+      }
     }
   }
 }
@@ -380,8 +394,8 @@ kvc_status kvc_cache_append(const kvc_cache* cache, const void* k_new, const voi
   if (lengths_out == nullptr) lengths_out = P.c.lengths;
   // (a head's new rows touch at most this many blocks, wherever its open block ends)
   const long long touched = ((long long)rows + P.c.block - 2) / P.c.block + 1;
-  // up to four blocks: one CTA per head, which can then write the length itself; more: a CTA per block
-  P.jobs_per_cta = touched <= 4 ? (int)touched : 1;
+  // up to four blocks: one CTA per head, which can then write the length itself; more: as many blocks as a CTA has jobs
+  P.jobs_per_cta = touched <= 4 ? (int)touched : job_cta_threads(P.c) / (P.c.block * P.c.d / 32);
   const long long steps = (touched + P.jobs_per_cta - 1) / P.jobs_per_cta;
   P.write_lengths = steps == 1 || lengths_out != P.c.lengths;
   const dim3 grid((unsigned)steps, P.c.units()), threads(job_cta_threads(P.c));

@@ -1,123 +1,224 @@
 // Eviction from an 8-bit cache by accumulated attention weight (kvc_evict).
 //
-// Two kernels.  evict_select_kernel, one CTA per head: the k-th largest of the weights before the protected rows is found
-// digit by digit (11, 11 and 10 bits of an order-preserving key, a histogram in shared memory each), then the kept
-// positions are written in order by counting along the row.  evict_move_kernel, a job per block of the new cache (see
-// cache8.cuh): kept rows are read once, take the exponent of their new block and are written once.
+// Two kernels.  evict_select_kernel, a cluster of up to eight CTAs per head: the weights before the protected rows are read
+// once into shared memory, as order-preserving keys, a share per CTA; the key of the last one to keep is found by counting how
+// many lie below seven places of the range that it is in, a third of a digit less each time (eleven steps at most; a
+// histogram of digits is fewer of them, but its atomics crowd into a few bins: 34 us for 64 heads of 32768 rows); the kept
+// positions are written in order.  evict_move_kernel, a job per block of the new cache (see cache8.cuh): kept rows are
+// read once, take the exponent of their new block and are written once.
 #include "cache8.cuh"
 
 namespace kvc {
 namespace {
 
-constexpr int kSelThreads = 1024;
-constexpr int kBins = 2048;
+constexpr int kSelThreads = 256;        // (1024: a step's barriers wait for 32 warps; 256 heads of 2112 rows 20 -> 53 us with one pivot)
+constexpr int kSelWarps = kSelThreads / 32;
+constexpr int kPivots = 7;
+constexpr int kSelKeep = 40960;         // keys that a CTA keeps in shared memory (160 KB); what is behind them is read again
+constexpr int kSelCluster = 8;
 
 struct EvictParams {
   Cache src, dst;
   long long budget, recent;
 };
 
-// Exclusive prefix sum over the CTA of a 0/1 flag, and the total; two barriers.
-__device__ __forceinline__ int flag_scan(bool flag, int* warp_sums, int* total) {
-  const uint32_t m = __ballot_sync(0xffffffffu, flag);
-  const int lane = threadIdx.x & 31, w = threadIdx.x >> 5;
-  if (lane == 0) warp_sums[w] = __popc(m);
+// What the CTAs of a cluster tell one another, by turns in two places.
+struct Exchange {
+  uint32_t warp[2][kSelWarps][8];
+  uint32_t cta[2][kSelCluster][8];
+};
+
+__device__ __forceinline__ uint32_t cluster_rank() {
+  uint32_t r;
+  asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+  return r;
+}
+
+// Sums of each of v's kN numbers over the CTA, left in x.cta[turn][rank] of every CTA of the cluster.
+template <int kN>
+__device__ __forceinline__ void tell(Exchange& x, int turn, uint32_t rank, int ctas, const uint32_t (&v)[kN]) {
+  const int tid = threadIdx.x;
+#pragma unroll
+  for (int j = 0; j < kN; ++j) {
+    const uint32_t sum = __reduce_add_sync(0xffffffffu, v[j]);
+    if ((tid & 31) == j) x.warp[turn][tid >> 5][j] = sum;
+  }
   __syncthreads();
-  const int mine = lane < kSelThreads / 32 ? warp_sums[lane] : 0;
-  const int before = __reduce_add_sync(0xffffffffu, lane < w ? mine : 0);
-  *total = __reduce_add_sync(0xffffffffu, mine);
-  __syncthreads();
-  return before + __popc(m & ((1u << lane) - 1u));
+  if (tid < 8 * ctas && (tid & 7) < kN) {
+    const int j = tid & 7;
+    uint32_t sum = 0;
+#pragma unroll
+    for (int w = 0; w < kSelWarps; ++w) sum += x.warp[turn][w][j];
+    const uint32_t mine = (uint32_t)__cvta_generic_to_shared(&x.cta[turn][rank][j]);
+    uint32_t theirs;
+    asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(theirs) : "r"(mine), "r"(tid >> 3));
+    asm volatile("st.shared::cluster.u32 [%0], %1;" :: "r"(theirs), "r"(sum) : "memory");
+  }
+  if (ctas == 1) {
+    __syncthreads();
+  } else {
+    __syncwarp();
+    asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+  }
 }
 
 __global__ void __launch_bounds__(kSelThreads)
-evict_select_kernel(const __grid_constant__ EvictParams P, const float* __restrict__ weight, int32_t* __restrict__ idx_out,
+evict_select_kernel(const __grid_constant__ EvictParams P, int ctas, const float* __restrict__ weight, int32_t* __restrict__ idx_out,
                     float* __restrict__ weight_out) {
-  __shared__ int hist[kBins];
-  __shared__ int warp_sums[kSelThreads / 32];
-  __shared__ int s_bin, s_before;
+  extern __shared__ __align__(16) uint32_t s_key[];
+  __shared__ Exchange x;
   grid_dependency_wait();
-  const int unit = blockIdx.x, tid = threadIdx.x;
-  const long long n = P.src.length(unit);
+  const uint32_t rank = ctas == 1 ? 0 : cluster_rank();
+  const int unit = blockIdx.x / ctas, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const int n = (int)P.src.length(unit), budget = (int)P.budget, recent = (int)P.recent;
   const float* w = weight + unit * P.src.cap;
   int32_t* idx = idx_out + unit * P.budget;
   float* wo = weight_out == nullptr ? nullptr : weight_out + unit * P.dst.cap;
-  const long long kept = n < P.budget ? n : P.budget;
-  if (tid == 0) P.dst.lengths[unit] = (int32_t)kept;
-  for (long long i = kept + tid; i < P.budget; i += kSelThreads) idx[i] = -1;
-  if (n <= P.budget) {
-    for (long long i = tid; i < n; i += kSelThreads) {
+  const int kept = min(n, budget), first = rank * kSelThreads + tid, step = ctas * kSelThreads;
+  if (first == 0) P.dst.lengths[unit] = kept;
+  for (long long i = kept + first; i < budget; i += step) idx[i] = -1;
+  if (n <= budget) {
+    for (long long i = first; i < n; i += step) {
       idx[i] = (int32_t)i;
       if (wo != nullptr) wo[i] = w[i];
     }
     return;
   }
-  // the heaviest `want` of the first `m` rows (keys ascend as weights descend)
-  const long long m = n - P.recent;
-  int want = (int)(P.budget - P.recent);
-  uint32_t prefix = 0;                  // the digits found so far
-  int ties = 0;                         // of the rows with exactly the threshold's key, the first `ties` are kept
-  if (want > 0) {
-    int shift = 32;
+  // behind the others: the protected rows
+  const int m = n - recent, want = budget - recent;
+  for (long long i = first; i < recent; i += step) {
+    idx[want + i] = (int32_t)(m + i);
+    if (wo != nullptr) wo[want + i] = w[m + i];
+  }
+  if (want == 0) return;
+
+  // this CTA's rows, in fours: row0 .. row0 + mine - 1, as keys that ascend as weights descend; padded with the largest key
+  const int each = (int)(((long long)m + 4 * ctas - 1) / (4 * ctas)) * 4;
+  const long long row0 = (long long)rank * each;
+  const int mine = (int)max(min((long long)each, m - row0), 0LL), held = min(mine, kSelKeep), fours = (held + 3) / 4;
+  w += row0;
+  for (int i0 = tid; i0 < 4 * fours; i0 += 8 * kSelThreads) {
+    float y[8];                                      // (eight loads in flight)
 #pragma unroll
-    for (int pass = 0; pass < 3; ++pass) {
-      const int bits = pass == 2 ? 10 : 11;
-      for (int i = tid; i < kBins; i += kSelThreads) hist[i] = 0;
-      __syncthreads();
-      const int up = shift;             // bits from `up` on are fixed
-      shift -= bits;
-      for (long long i = tid; i < m; i += kSelThreads) {
-        const uint32_t key = score_to_key(w[i]);
-        if (pass == 0 || (key >> up) == (prefix >> up)) atomicAdd(&hist[(key >> shift) & ((1 << bits) - 1)], 1);
-      }
-      __syncthreads();
-      // the bin that the want-th row falls into: two bins per thread, scanned over the CTA
-      const int a = hist[2 * tid], b = hist[2 * tid + 1];
-      int x = a + b;
+    for (int u = 0; u < 8; ++u) y[u] = i0 + u * kSelThreads < held ? __ldg(w + i0 + u * kSelThreads) : 0.f;
 #pragma unroll
-      for (int o = 1; o < 32; o <<= 1) {
-        const int y = __shfl_up_sync(0xffffffffu, x, o);
-        if ((tid & 31) >= o) x += y;
-      }
-      if ((tid & 31) == 31) warp_sums[tid >> 5] = x;
-      __syncthreads();
-      const int other = warp_sums[tid & 31];
-      const int before = __reduce_add_sync(0xffffffffu, (tid & 31) < (tid >> 5) ? other : 0) + x - a - b;
-      if (before < want && want <= before + a + b) {
-        const int first = want <= before + a;
-        s_bin = first ? 2 * tid : 2 * tid + 1;
-        s_before = first ? before : before + a;
-      }
-      __syncthreads();
-      prefix |= (uint32_t)s_bin << shift;
-      want -= s_before;
-      __syncthreads();
+    for (int u = 0; u < 8; ++u) {
+      const int i = i0 + u * kSelThreads;
+      if (i < 4 * fours) s_key[i] = i < held ? score_to_key(y[u]) : 0xffffffffu;
     }
-    ties = want;
   }
-  // positions in order
-  long long done = 0;
-  int ties_done = 0;
-  for (long long i0 = 0; i0 < m; i0 += kSelThreads) {
-    const long long i = i0 + tid;
-    const float x = i < m ? w[i] : 0.f;
-    const uint32_t key = score_to_key(x);
-    const bool equal = i < m && ties > 0 && key == prefix;
-    int total;
-    const int rank = flag_scan(equal, warp_sums, &total) + ties_done;
-    const bool keep = i < m && ties > 0 && (key < prefix || (equal && rank < ties));
-    ties_done += total;
-    const int at = flag_scan(keep, warp_sums, &total);
-    if (keep) {
-      idx[done + at] = (int32_t)i;
-      if (wo != nullptr) wo[done + at] = x;
+  __syncthreads();
+
+  // The smallest key that at least `want` rows do not exceed lies in [low, hi].
+  const uint4* fours_of = reinterpret_cast<const uint4*>(s_key);
+  uint32_t low = 0, hi = 0xffffffffu;
+  int low_count = 0, ties = -1, turn = 0;            // rows below `low`; of the rows with the last key, the first `ties` are kept
+  if (ctas > 1)                                      // (a CTA's shared memory is written to by the others once all of them run)
+    asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+  while (low < hi) {
+    const uint32_t range = hi - low, stride = (range >> 3) + 1;
+    uint32_t pivot[kPivots], count[kPivots];         // places in (low, hi], keys below them
+#pragma unroll
+    for (int j = 0; j < kPivots; ++j) {
+      pivot[j] = low + min(stride * (j + 1), range);
+      count[j] = 0;
     }
-    done += total;
+    for (int i = tid; i < fours; i += kSelThreads) {
+      const uint4 k = fours_of[i];
+#pragma unroll
+      for (int j = 0; j < kPivots; ++j) count[j] += (k.x < pivot[j]) + (k.y < pivot[j]) + (k.z < pivot[j]) + (k.w < pivot[j]);
+    }
+    for (long long i = held + tid; i < mine; i += kSelThreads) {
+      const uint32_t key = score_to_key(w[i]);
+#pragma unroll
+      for (int j = 0; j < kPivots; ++j) count[j] += key < pivot[j];
+    }
+    tell(x, turn, rank, ctas, count);
+    uint32_t total = 0;                              // lane j: of pivot j
+    if (lane < kPivots)
+      for (int c = 0; c < ctas; ++c) total += x.cta[turn][c][lane];
+    turn ^= 1;
+    const uint32_t exact = __ballot_sync(0xffffffffu, lane < kPivots && (int)total == want);
+    const int below = __popc(__ballot_sync(0xffffffffu, lane < kPivots && (int)total < want));      // (counts do not fall with the pivots)
+    const uint32_t from = low;
+    if (exact != 0) {                                // all keys below that pivot are kept
+      hi = from + min(stride * __ffs(exact), range) - 1;
+      ties = 0x7fffffff;
+      break;
+    }
+    if (below < kPivots) hi = from + min(stride * (below + 1), range) - 1;
+    if (below > 0) {
+      low = from + min(stride * below, range);
+      low_count = (int)__shfl_sync(0xffffffffu, total, below - 1);
+    }
   }
-  for (long long i = tid; i < P.recent; i += kSelThreads) {
-    idx[P.budget - P.recent + i] = (int32_t)(m + i);
-    if (wo != nullptr) wo[P.budget - P.recent + i] = w[m + i];
+  if (ties < 0) ties = want - low_count;
+
+  // Positions in order.  A row in front of which lie l rows with smaller keys and q with the last key goes to place
+  // l + min(q, ties).
+  uint32_t both[2] = {0, 0};
+  for (int i = tid; i < fours; i += kSelThreads) {
+    const uint4 k = fours_of[i];
+    both[0] += (k.x < hi) + (k.y < hi) + (k.z < hi) + (k.w < hi);
+    const int at = 4 * i;
+    both[1] += (k.x == hi && at < held) + (k.y == hi && at + 1 < held) + (k.z == hi && at + 2 < held) + (k.w == hi && at + 3 < held);
   }
+  for (long long i = held + tid; i < mine; i += kSelThreads) {
+    const uint32_t key = score_to_key(w[i]);
+    both[0] += key < hi;
+    both[1] += key == hi;
+  }
+  tell(x, turn, rank, ctas, both);
+  int less = 0, equal = 0;
+  for (uint32_t c = 0; c < rank; ++c) {
+    less += x.cta[turn][c][0];
+    equal += x.cta[turn][c][1];
+  }
+  for (long long i0 = 0; i0 < mine; i0 += 4 * kSelThreads) {     // four rows in a row per thread
+    const long long at = i0 + 4 * tid;
+    uint32_t key[4];
+    int flags = 0;                                   // smaller keys; equal ones, 2^16 times
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      key[u] = 0xffffffffu;
+      if (at + u >= mine) continue;
+      key[u] = at + u < held ? s_key[at + u] : score_to_key(w[at + u]);
+      flags += (key[u] < hi ? 1 : 0) + (key[u] == hi ? 1 << 16 : 0);
+    }
+    int incl = flags;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int y = __shfl_up_sync(0xffffffffu, incl, o);
+      if (lane >= o) incl += y;
+    }
+    turn ^= 1;                                       // (one barrier per step: the sums of the step before are in the other place)
+    if (lane == 31) x.warp[turn][warp][0] = incl;
+    __syncthreads();
+    const int other = lane < kSelWarps ? x.warp[turn][lane][0] : 0;
+    const int before = __reduce_add_sync(0xffffffffu, lane < warp ? other : 0) + incl - flags;
+    const int all = __reduce_add_sync(0xffffffffu, other);
+    int l = less + (before & 0xffff), q = equal + (before >> 16);
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      if (at + u >= mine) continue;
+      if (key[u] < hi || (key[u] == hi && q < ties)) {
+        const int place = l + min(q, ties);
+        idx[place] = (int32_t)(row0 + at + u);
+        if (wo != nullptr) wo[place] = w[at + u];
+      }
+      l += key[u] < hi;
+      q += key[u] == hi;
+    }
+    less += all & 0xffff;
+    equal += all >> 16;
+  }
+}
+
+// CTAs per head: as many as keep the keys in shared memory, and as fit the GPU at once (four per SM) if they have 4096 keys each.
+int select_ctas(long long cap, long long units, int sms) {
+  int c = 1;
+  while (c < kSelCluster && (cap > (long long)c * kSelKeep || (units * c * 2 <= 4 * sms && cap > (long long)c * 4096))) c *= 2;
+  return c;
 }
 
 template <int kFormat>
@@ -211,7 +312,26 @@ extern "C" kvc_status kvc_evict(const kvc_cache* src, const kvc_cache* dst, cons
   if ((s = require_device()) != KVC_OK) return s;
   P.budget = budget; P.recent = recent;
   cudaStream_t st = (cudaStream_t)stream;
-  KVC_CUDA(launch_dependent(evict_select_kernel, dim3((unsigned)U), dim3(kSelThreads), 0, st, P, weight, idx_out, weight_out));
+  int dev = 0, sms = 0;
+  KVC_CUDA(cudaGetDevice(&dev));
+  KVC_CUDA(cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev));
+  const int ctas = select_ctas(a.cap, U, sms);
+  const long long each = ((a.cap + 4 * ctas - 1) / (4 * ctas)) * 4;
+  KVC_CUDA(cudaFuncSetAttribute(evict_select_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSelKeep * 4));
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = ctas;
+  attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)(U * ctas));
+  cfg.blockDim = dim3(kSelThreads);
+  cfg.dynamicSmemBytes = (size_t)(each < kSelKeep ? each : kSelKeep) * 4;
+  cfg.stream = st;
+  cfg.attrs = attr;
+  cfg.numAttrs = 2;
+  KVC_CUDA(cudaLaunchKernelEx(&cfg, evict_select_kernel, P, ctas, weight, idx_out, weight_out));
   KVC_LAUNCH_CHECK("evict_select_kernel");
   const int threads = job_cta_threads(b);
   const long long per_cta = (long long)(threads / (b.block * b.d / 32)) * b.block;
