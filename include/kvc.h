@@ -373,7 +373,7 @@ typedef struct {
   int32_t block;             /* tokens per exponent: 16, 32, 64 or 128 */
   int32_t format;            /* kvc_cache_format */
   int32_t reserved_;         /* must be 0 */
-  int64_t capacity;          /* rows a head has room for, 1 <= capacity < 2^31 - 128 */
+  int64_t capacity;          /* rows a head has room for, 1 <= capacity < 2^31 - 1024 */
   int64_t stride[3];         /* strides of k and v in codes (batch, head, token), multiples of 16; 0 in slot 0: dense */
   void* k;                   /* [batch, n_kv_heads, capacity, head_dim], one byte per code; 16-byte aligned */
   void* v;

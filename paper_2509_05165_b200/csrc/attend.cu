@@ -19,9 +19,10 @@
 // Numbers: codes are exact in fp16.  A query row is scaled by a power of two to below 2 and rounded to fp16, which is exact
 // for bf16 but for entries 2^14 times smaller than the row's largest; fp32 rows go as two fp16 (22 bits), and so does P in
 // front of V then (one fp16, 11 bits, for bf16 outputs).  Products, softmax and sums are fp32.  V's exponents differ from block
-// to block: P goes in relative to 2^M, M the running maximum of logit + exponent, which keeps the largest terms of a row at
-// full precision whatever block they are in, and 2^15 times larger, so that 2^17 weights of 2^-26 are not lost beside one
-// of 1/2, as they are in an fp16 of at most 1.
+// to block: P goes in relative to 2^M, M a running maximum of logit + exponent, which keeps the largest terms of a row at
+// full precision whatever block they are in, and 2^5 times larger, so that 2^17 weights of 2^-26 are not lost beside one of
+// 1/2, as they are in an fp16 of at most 1.  References only move when they are exceeded by 2^10 (2^60 for the sums): until
+// then no lane needs another's maximum (with a maximum per step, four rows over 128K tokens 79 -> XX us).
 #include <math.h>
 
 #include "cache8.cuh"
@@ -34,7 +35,7 @@ constexpr int kSetup = 2;                 // granules that a head's start counts
 constexpr int kMaxWarps = 12;
 constexpr int kMaxCtas = 256;             // bounds the workspace, whatever the device
 constexpr int kMaxRows = 64;              // query rows of a KV head that one launch takes (bounds the logits kept)
-constexpr float kLift = 15.f;             // P goes into V as 2^15 p: fp16 then tells weights apart down to 2^-40 of the largest
+constexpr float kSlackSum = 60.f;         // logits may exceed the reference of the sums by this much (see Form for V's)
 constexpr float kNone = -3e38f;           // "no logit yet": finite, so that differences are numbers
 constexpr int kJoinThreads = 128;
 constexpr int kJoinTokens = 512;
@@ -138,6 +139,9 @@ struct Shares {
 template <typename T, int kD, int kTiles>
 struct Form {
   static constexpr bool kTwo = sizeof(T) == 4;         // fp32: Q and P as two fp16 each
+  // P goes into V as 2^kLift p, relative to a reference that it may exceed by 2^kSlack: 2^15 fits fp16, and its smallest steps are
+  // 2^-29 of the row's largest weight (fp32: 2^-36, at the price of references that move more often)
+  static constexpr float kLift = kTwo ? 12.f : 5.f, kSlack = kTwo ? 3.f : 10.f;
   static constexpr bool kQShared = kTiles == 4;        // Q's operands in shared memory (else in registers)
   static constexpr int kWarps = kTiles == 1 ? 12 : kTiles == 2 && !kTwo ? 10 : 8;
   static constexpr int kThreads = kWarps * 32;
@@ -308,16 +312,14 @@ attend_split_kernel(const __grid_constant__ AttendParams P, const T* __restrict_
 #pragma unroll
     for (int s = 0; s < kStages - 1; ++s) fetch(s);
 
-    // exponents of the two halves of 32 tokens, read one step ahead
-    int ek[2], ev[2], ek_next[2] = {0, 0}, ev_next[2] = {0, 0};
+    // exponents of the two halves of 32 tokens, K's and V's: a lane reads those of one step in 32, four bytes in one register
+    uint32_t exps = 0;
     auto fetch_exps = [&](int it) {
-#pragma unroll
-      for (int f = 0; f < 2; ++f) {
-        const int tok = first + it * stride + 16 * f;
-        if (it < iters && tok < hi) {
-          ek_next[f] = __ldg(ke + (tok >> c.block_shift));
-          ev_next[f] = __ldg(ve + (tok >> c.block_shift));
-        }
+      const int tok = first + (it + lane) * stride;
+      if (it + lane < iters) {
+        const int at0 = tok >> c.block_shift, at1 = min(tok + 16, hi - 1) >> c.block_shift;
+        exps = (uint32_t)(uint8_t)__ldg(ke + at0) | (uint32_t)(uint8_t)__ldg(ke + at1) << 8 | (uint32_t)(uint8_t)__ldg(ve + at0) << 16 |
+               (uint32_t)(uint8_t)__ldg(ve + at1) << 24;
       }
     };
     fetch_exps(0);
@@ -392,8 +394,9 @@ attend_split_kernel(const __grid_constant__ AttendParams P, const T* __restrict_
     if (kWeight) logit_row = P.logits + ((long long)unit * P.row_tiles + rt) * c.cap * P.logit_rows + 2 * t;
 
     for (int it = 0; it < iters; ++it) {
-      ek[0] = ek_next[0]; ek[1] = ek_next[1]; ev[0] = ev_next[0]; ev[1] = ev_next[1];
-      fetch_exps(it + 1);
+      if (it > 0 && (it & 31) == 0) fetch_exps(it);
+      const uint32_t four = __shfl_sync(0xffffffffu, exps, it & 31);
+      const int ek[2] = {(int8_t)four, (int8_t)(four >> 8)}, ev[2] = {(int8_t)(four >> 16), (int8_t)(four >> 24)};
       fetch(it + kStages - 1);
       copy_wait<kStages - 1>();
       const char* stage = my_smem + (it % kStages) * F::kStageBytes;
@@ -472,44 +475,42 @@ attend_split_kernel(const __grid_constant__ AttendParams P, const T* __restrict_
           }
       }
 
-      // ---- running maxima of the logits and of logit + V's exponent; sums and outputs follow them
-      const bool same = ev[0] == ev[1];
+      // ---- references of the logits and of logit + V's exponent.  They move when a lane finds one exceeded by more than the slack:
+      // then to the maxima of these tokens over all lanes, and sums and outputs follow.
+      const float evf[2] = {(float)ev[0], (float)ev[1]};
+      float over = -INFINITY;
 #pragma unroll
-      for (int n = 0; n < kTiles; ++n) {
-        float ms[2], mv[2];
+      for (int n = 0; n < kTiles; ++n)
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
-          float m0 = fmaxf(sc[0][n][i], sc[0][n][2 + i]), m1 = fmaxf(sc[1][n][i], sc[1][n][2 + i]);
-          if (same) {
-            m0 = fmaxf(m0, m1);
-#pragma unroll
-            for (int x = 4; x < 32; x <<= 1) m0 = fmaxf(m0, __shfl_xor_sync(0xffffffffu, m0, x));
-            m1 = m0;
-          } else {
-#pragma unroll
-            for (int x = 4; x < 32; x <<= 1) {
-              m0 = fmaxf(m0, __shfl_xor_sync(0xffffffffu, m0, x));
-              m1 = fmaxf(m1, __shfl_xor_sync(0xffffffffu, m1, x));
-            }
-          }
-          ms[i] = fmaxf(top_s[n][i], fmaxf(m0, m1));
-          mv[i] = fmaxf(top_v[n][i], fmaxf(m0 + ev[0], m1 + ev[1]));
+          const float m0 = fmaxf(sc[0][n][i], sc[0][n][2 + i]), m1 = fmaxf(sc[1][n][i], sc[1][n][2 + i]);
+          over = fmaxf(over, fmaxf(m0 + evf[0], m1 + evf[1]) - top_v[n][i] - F::kSlack);
+          over = fmaxf(over, fmaxf(m0, m1) - top_s[n][i] - kSlackSum);
         }
-        const bool grew = ms[0] > top_s[n][0] || ms[1] > top_s[n][1] || mv[0] > top_v[n][0] || mv[1] > top_v[n][1];
-        if (__any_sync(0xffffffffu, grew)) {
+      if (__any_sync(0xffffffffu, over > 0.f)) {
+#pragma unroll
+        for (int n = 0; n < kTiles; ++n)
 #pragma unroll
           for (int i = 0; i < 2; ++i) {
-            sum[n][i] *= ex2(top_s[n][i] - ms[i]);
-            const float r = ex2(top_v[n][i] - mv[i]);
+            const float m0 = fmaxf(sc[0][n][i], sc[0][n][2 + i]), m1 = fmaxf(sc[1][n][i], sc[1][n][2 + i]);
+            float ms = fmaxf(m0, m1), mv = fmaxf(m0 + evf[0], m1 + evf[1]);
+#pragma unroll
+            for (int x = 4; x < 32; x <<= 1) {
+              ms = fmaxf(ms, __shfl_xor_sync(0xffffffffu, ms, x));
+              mv = fmaxf(mv, __shfl_xor_sync(0xffffffffu, mv, x));
+            }
+            ms = fmaxf(ms, top_s[n][i]);
+            mv = fmaxf(mv, top_v[n][i]);
+            sum[n][i] *= ex2(top_s[n][i] - ms);
+            const float r = ex2(top_v[n][i] - mv);
 #pragma unroll
             for (int s = 0; s < kSteps; ++s) {
               o[n][s][i] *= r;
               o[n][s][2 + i] *= r;
             }
-            top_s[n][i] = ms[i];
-            top_v[n][i] = mv[i];
+            top_s[n][i] = ms;
+            top_v[n][i] = mv;
           }
-        }
       }
 
       // ---- P, and its share of the outputs
@@ -520,8 +521,8 @@ attend_split_kernel(const __grid_constant__ AttendParams P, const T* __restrict_
         for (int n = 0; n < kTiles; ++n) {
           float up[2];
 #pragma unroll
-          for (int i = 0; i < 2; ++i) up[i] = top_s[n][i] + ev[f] - top_v[n][i] + kLift;
-          const bool far = fmaxf(up[0], up[1]) > 126.f;         // (V's exponents more than 2^111 apart: the factor is no fp32)
+          for (int i = 0; i < 2; ++i) up[i] = top_s[n][i] + evf[f] - top_v[n][i] + F::kLift;
+          const bool far = fmaxf(up[0], up[1]) > 100.f;         // (V's exponents so far apart that p may be no fp32 where its product is)
           up[0] = ex2(up[0]);
           up[1] = ex2(up[1]);
           float p[4];
@@ -533,7 +534,7 @@ attend_split_kernel(const __grid_constant__ AttendParams P, const T* __restrict_
           }
           if (far) {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) p[i] = ex2(sc[f][n][i] + (ev[f] - top_v[n][i & 1] + kLift));
+            for (int i = 0; i < 4; ++i) p[i] = ex2(sc[f][n][i] + (evf[f] - top_v[n][i & 1] + F::kLift));
           }
 #pragma unroll
           for (int i = 0; i < 2; ++i) {
@@ -592,7 +593,7 @@ attend_split_kernel(const __grid_constant__ AttendParams P, const T* __restrict_
         for (int i = 0; i < 2; ++i) {
           const int row = 8 * n + 2 * t + i;
           if (row < live_rows) {
-            const float r = ex2(top_v[n][i] - kLift - top_s[n][i]);
+            const float r = ex2(top_v[n][i] - F::kLift - top_s[n][i]);
             float* dst = P.part_o + (slot * kRows + row) * kD + 4 * g;
 #pragma unroll
             for (int k = 0; k < kSteps / 2; ++k)
@@ -622,7 +623,7 @@ attend_split_kernel(const __grid_constant__ AttendParams P, const T* __restrict_
           float m = s_stat[0][row][0];
 #pragma unroll
           for (int w = 1; w < kWarps; ++w) m = fmaxf(m, s_stat[w][row][0]);
-          const float r = ex2(top_v[n][i] - kLift - m);
+          const float r = ex2(top_v[n][i] - F::kLift - m);
           float* dst = so + (warp * kRows + row) * kPitch + 4 * g;
 #pragma unroll
           for (int k = 0; k < kSteps / 2; ++k)

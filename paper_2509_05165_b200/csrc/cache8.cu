@@ -330,7 +330,7 @@ kvc_status resolve_cache(const kvc_cache* c, const char* name, Cache* out) {
   KVC_REQUIRE8(c->format == KVC_INT8 || c->format == KVC_E4M3, KVC_ERR_INVALID_ARG, "%s: unknown format", name);
   KVC_REQUIRE8(c->reserved_ == 0, KVC_ERR_INVALID_ARG, "%s: reserved_ must be 0", name);
   KVC_REQUIRE8(c->capacity >= 1, KVC_ERR_INVALID_ARG, "%s: capacity must be >= 1", name);
-  KVC_REQUIRE8(c->capacity < (1LL << 31) - 128, KVC_ERR_UNSUPPORTED, "%s: capacity must be < 2^31 - 128", name);
+  KVC_REQUIRE8(c->capacity < (1LL << 31) - 1024, KVC_ERR_UNSUPPORTED, "%s: capacity must be < 2^31 - 1024", name);
   KVC_REQUIRE8(c->k && c->v && c->k_exp && c->v_exp && c->lengths, KVC_ERR_INVALID_ARG, "%s: k, v, k_exp, v_exp or lengths is NULL", name);
   KVC_REQUIRE8(aligned16(c->k) && aligned16(c->v), KVC_ERR_INVALID_ARG, "%s: k or v is not 16-byte aligned", name);
   KVC_REQUIRE8((reinterpret_cast<uintptr_t>(c->lengths) & 3u) == 0, KVC_ERR_INVALID_ARG, "%s: lengths is not 4-byte aligned", name);

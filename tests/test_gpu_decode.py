@@ -292,11 +292,11 @@ def _check_attend(c, q, out, lse, weight, weight0, causal, scale, counts=None):
     rounded to 11 bits in front of V and the sum to bf16; fp32: p to 22 bits and the sums of up to thousands of terms, kept in
     fp32 by parts, within 2^-19."""
     k, v = _clean_values(c)
-    # P 2^15 in fp16 (or, for fp32, what is left of it after the first fp16), relative to the row's largest p 2^e: numbers below
-    # 2^-14 have steps of 2^-24, so p 2^e is off by up to half of 2^-39 of that largest one, for codes of up to 448
+    # P 2^5 (fp32: 2^12) in fp16, relative to a p 2^e of at most the row's largest: numbers below 2^-14 have steps of 2^-24, so p 2^e is
+    # off by up to half of 2^-29 (2^-36) of that largest one, for codes of up to 448
     step = torch.pow(torch.tensor(2.0, dtype=torch.float64), c.v_exp.cpu().double()).repeat_interleave(c.block, -1)[..., :c.capacity]
     rel = 2.0 ** -11 if q.dtype == BF else 2.0 ** -19
-    o, l, w, mass, size = R.attend(q.cpu().double(), k, v, c.lengths.cpu(), causal, scale, counts, step, 2.0 ** -39 / rel)
+    o, l, w, mass, size = R.attend(q.cpu().double(), k, v, c.lengths.cpu(), causal, scale, counts, step, 2.0 ** (-29 if q.dtype == BF else -36) / rel)
     dp = 2 * (2.0 ** -19 * size + 2.0 ** -19)
     bf = q.dtype == BF
     got = out.cpu().double()
