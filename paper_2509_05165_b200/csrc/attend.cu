@@ -1,6 +1,6 @@
 // Attention of a few query rows over an 8-bit cache (kvc_attend).
 //
-// HBM is the bound: 2 d bytes of codes per token and KV head, against 4 d products per query row.  Two kernels:
+// HBM is the bound: 2 d bytes of codes per token and KV head, against 4 d products per query row.  Two kernels, three with weights:
 //
 // attend_split_kernel   one CTA per SM.  The tokens of all heads, in granules of kGranule (and kSetup granules more per head,
 //   for what starting one costs), are laid end to end and cut into equal shares, one per CTA, whatever the lengths.  A CTA
@@ -13,8 +13,9 @@
 //   of its tokens of V as its rows; a transpose of P's 8 x 8 tiles (movmatrix) is the only exchange between lanes.  Legacy
 //   mma on purpose: an SM scheduler has 44 clocks per token before the codes arrive from HBM and mma takes 8 of them (8.0 clk
 //   per m16n8k16, measured); through tcgen05 the converted codes would have to go back to shared memory first.
-// attend_join_kernel    joins the parts of a row (log-sum-exp), and adds the row's weights from the logits, which the first
-//   kernel leaves in the workspace (they stay in L2; the softmax's denominator is known only after the last token).
+// attend_join_kernel    joins the parts of a row (log-sum-exp).
+// attend_weight_kernel  adds the rows' weights from the logits, which the first kernel leaves in the workspace (they stay in L2; the
+//   softmax's denominator is known only after the last token).
 //
 // Numbers: codes are exact in fp16.  A query row is scaled by a power of two to below 2 and rounded to fp16, which is exact
 // for bf16 but for entries 2^14 times smaller than the row's largest; fp32 rows go as two fp16 (22 bits), and so does P in
@@ -37,8 +38,10 @@ constexpr int kMaxCtas = 256;             // bounds the workspace, whatever the 
 constexpr int kMaxRows = 64;              // query rows of a KV head that one launch takes (bounds the logits kept)
 constexpr float kSlackSum = 60.f;         // logits may exceed the reference of the sums by this much (see Form for V's)
 constexpr float kNone = -3e38f;           // "no logit yet": finite, so that differences are numbers
-constexpr int kJoinThreads = 128;
-constexpr int kJoinTokens = 512;
+constexpr int kJoinThreads = 256;
+constexpr int kJoinWarps = kJoinThreads / 32;
+constexpr int kJoinEach = 4;              // tokens of a thread
+constexpr int kJoinTokens = kJoinThreads * kJoinEach;
 
 struct AttendParams {
   Cache c;
@@ -50,6 +53,7 @@ struct AttendParams {
   float* part_o;                          // [slot][tile_rows][d]
   float2* part_ml;                        // [slot][tile_rows]: largest logit (in powers of two), sum of 2^(logit - it)
   float* logits;                          // [unit][row tile][token][logit_rows]
+  float* lse2;                            // [unit][live]
   long long* before;                      // [units + 1]: granules (with kSetup) in front of a head, per row tile; all of them last
 };
 
@@ -172,7 +176,6 @@ attend_split_kernel(const __grid_constant__ AttendParams P, const T* __restrict_
   __shared__ float s_stat[kWarps][kRows][2];
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t = lane & 3;
   grid_dependency_wait();
-  asm volatile("griddepcontrol.launch_dependents;");   // (attend_join_kernel may come up; it waits for this grid's end itself)
   const Cache& c = P.c;
   const int units = c.units();
 
@@ -698,108 +701,132 @@ __device__ __forceinline__ Parts parts_of(const AttendParams& P, int unit, int r
   return r;
 }
 
-// One warp: the largest logit of a row over its parts, and the sum of 2^(logit - it).
-__device__ __forceinline__ float2 join_stats(const AttendParams& P, const Parts& r, int row) {
-  const int lane = threadIdx.x & 31, n = r.count();
-  float m = kNone, l = 0.f;
-  for (int i = lane; i < n; i += 32) {                 // (a running sum: each part is read once)
-    const float2 a = P.part_ml[r[i] * P.tile_rows + row];
-    const float top = fmaxf(m, a.x);
-    l = l * ex2(m - top) + a.y * ex2(a.x - top);
-    m = top;
-  }
-#pragma unroll
-  for (int x = 1; x < 32; x <<= 1) {
-    const float m2 = __shfl_xor_sync(0xffffffffu, m, x), l2 = __shfl_xor_sync(0xffffffffu, l, x);
-    const float top = fmaxf(m, m2);
-    l = l * ex2(m - top) + l2 * ex2(m2 - top);
-    m = top;
-  }
-  return make_float2(m, l);
-}
-
-// The first units * live CTAs write a query row's output each; the others add the weights of kJoinTokens tokens of a head.
+// A CTA writes 2^row_shift query rows' outputs of a head, and their log-sum-exps in powers of two for attend_weight_kernel.  The
+// warps share the rows out; a warp takes every so many-th part of its row (of 64 entries: two parts at a time), statistics and
+// output in one go, against a running maximum, and the warps meet once.
 template <typename T, int kD>
 __global__ void __launch_bounds__(kJoinThreads)
 attend_join_kernel(const __grid_constant__ AttendParams P, const int32_t* __restrict__ row_counts, T* __restrict__ out,
-                   float* __restrict__ lse, const float* weight_in, float* weight_out, int chunks) {
-  __shared__ float s_lse[kMaxRows];
-  __shared__ float4 s_o[kJoinThreads / 32][32];
+                   float* __restrict__ lse, int row_shift) {
+  constexpr int kLanes = kD / 4;                       // lanes of a part's row, 16 bytes each
+  constexpr int kPer = 32 / kLanes;                    // parts a warp reads side by side
+  constexpr int kGroups = kJoinWarps * kPer;
+  __shared__ float2 s_ml[kGroups];
+  __shared__ float4 s_o[kGroups][kLanes];
   grid_dependency_wait();
   const Cache& c = P.c;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, units = c.units();
-  const bool is_row = blockIdx.x < (unsigned)(units * P.live);
-  const int job = is_row ? blockIdx.x : blockIdx.x - units * P.live;
-  const int unit = is_row ? job / P.live : job / chunks;
-  const long long len = c.length(unit);
-  const long long tok0 = is_row ? 0 : (long long)(job - unit * chunks) * kJoinTokens;
-  if (!is_row && tok0 >= len) return;
-  const int b = unit / c.Hkv, h = unit - b * c.Hkv;
-  const int rows = row_count(P, row_counts, b);
-
-  if (is_row) {
-    const int r = job - unit * P.live, rr = P.row0 + r, rt = r / P.tile_rows, row = r - rt * P.tile_rows;
-    const int m = rr % P.rows, j = h * P.G + rr / P.rows;
-    if (m >= rows) return;                           // a row that the sequence has not got
-    const Parts parts = parts_of(P, unit, rt);
-    const float2 ml = join_stats(P, parts, row);     // (every warp for itself)
-    constexpr int kLanes = kD / 4;                   // lanes of a part's row, 16 bytes each
-    constexpr int kPer = 32 / kLanes;                // parts a warp reads side by side
-    const int x = lane % kLanes;
-    float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 4
-    for (int i = warp * kPer + lane / kLanes; i < parts.count(); i += kPer * (kJoinThreads / 32)) {
-      const long long s = parts[i];
-      const float4 y = *reinterpret_cast<const float4*>(P.part_o + (s * P.tile_rows + row) * kD + 4 * x);
-      const float f = ex2(P.part_ml[s * P.tile_rows + row].x - ml.x);
-      a.x += y.x * f; a.y += y.y * f; a.z += y.z * f; a.w += y.w * f;
-    }
-    s_o[warp][lane] = a;
-    __syncthreads();
-    if (tid < kLanes) {
-      for (int w = 0; w < kJoinThreads / 32; ++w)
+  const int per_unit = (P.live + (1 << row_shift) - 1) >> row_shift, unit = blockIdx.x / per_unit;
+  const int r0 = (blockIdx.x - unit * per_unit) << row_shift;
+  const int x = lane % kLanes, group = warp * kPer + lane / kLanes, groups = kGroups >> row_shift;      // of a row
+  const int r = r0 + group / groups, rt = min(r, P.live - 1) / P.tile_rows, row = min(r, P.live - 1) - rt * P.tile_rows;
+  const Parts parts = parts_of(P, unit, rt);
+  const int n = parts.count();
+  float m = kNone, l = 0.f;
+  float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
+  for (int i0 = group % groups; i0 < n; i0 += 4 * groups) {      // four parts in flight
+    float2 ml[4];
+    float4 y[4];
 #pragma unroll
-        for (int k = 0; k < kPer; ++k) {
-          if (w + k == 0) continue;
-          const float4 y = s_o[w][tid + k * kLanes];
-          a.x += y.x; a.y += y.y; a.z += y.z; a.w += y.w;
-        }
-      const float inv = ml.y > 0.f ? 1.f / ml.y : 0.f;
-      // place 8 k + g holds entries (kD / 8) g + 4 k ..
-      T* dst = out + b * P.os[0] + j * P.os[1] + m * P.os[2] + (kD / 8) * (tid & 7) + 4 * (tid >> 3);
-      a.x *= inv; a.y *= inv; a.z *= inv; a.w *= inv;
-      if (sizeof(T) == 2) {
-        const __nv_bfloat162 lo = __floats2bfloat162_rn(a.x, a.y), hi = __floats2bfloat162_rn(a.z, a.w);
-        *reinterpret_cast<uint2*>(dst) = make_uint2(*reinterpret_cast<const uint32_t*>(&lo), *reinterpret_cast<const uint32_t*>(&hi));
-      } else {
-        *reinterpret_cast<float4*>(dst) = a;
+    for (int k = 0; k < 4; ++k) {
+      const int i = i0 + k * groups;
+      ml[k] = make_float2(kNone, 0.f);
+      y[k] = make_float4(0.f, 0.f, 0.f, 0.f);
+      if (i < n) {
+        const long long at = parts[i] * P.tile_rows + row;
+        ml[k] = P.part_ml[at];
+        y[k] = *reinterpret_cast<const float4*>(P.part_o + at * kD + 4 * x);
       }
-      if (tid == 0 && lse != nullptr)
-        lse[((long long)b * P.Hq + j) * P.rows + m] = ml.y > 0.f ? (ml.x + log2f(ml.y)) * 0.693147180559945309f : -INFINITY;
     }
-    return;
+    const float top = fmaxf(m, fmaxf(fmaxf(ml[0].x, ml[1].x), fmaxf(ml[2].x, ml[3].x)));
+    const float down = ex2(m - top);
+    l *= down; a.x *= down; a.y *= down; a.z *= down; a.w *= down;
+    m = top;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const float f = ex2(ml[k].x - top);
+      l += ml[k].y * f;
+      a.x += y[k].x * f; a.y += y[k].y * f; a.z += y[k].z * f; a.w += y[k].w * f;
+    }
   }
-
-  // ---- weights: the logits' log-sum-exps, then the tokens
-  for (int r = warp; r < P.live; r += kJoinThreads / 32) {
-    const int rt = r / P.tile_rows;
-    const float2 ml = join_stats(P, parts_of(P, unit, rt), r - rt * P.tile_rows);
-    if (lane == 0) s_lse[r] = ml.y > 0.f && (P.row0 + r) % P.rows < rows ? ml.x + log2f(ml.y) : INFINITY;     // (infinity: weighs nothing)
-  }
+  s_o[group][x] = a;
+  if (x == 0) s_ml[group] = make_float2(m, l);
   __syncthreads();
-  for (long long tok = tok0 + tid; tok < min(tok0 + kJoinTokens, len); tok += kJoinThreads) {
-    float w = 0.f;
+  // thread: an output's 16 bytes
+  const int out_row = tid / kLanes, at = tid - out_row * kLanes, r1 = r0 + out_row;
+  const int b = unit / c.Hkv, h = unit - b * c.Hkv;
+  const int rr = P.row0 + r1, j = h * P.G + rr / P.rows, mm = rr % P.rows;
+  if (out_row >= 1 << row_shift || r1 >= P.live || mm >= row_count(P, row_counts, b)) return;      // (rows that the sequence has not got stay as they are)
+  float top = kNone;
+  for (int k = out_row * groups; k < (out_row + 1) * groups; ++k) top = fmaxf(top, s_ml[k].x);
+  l = 0.f;
+  a = make_float4(0.f, 0.f, 0.f, 0.f);
+  for (int k = out_row * groups; k < (out_row + 1) * groups; ++k) {
+    const float2 ml = s_ml[k];
+    const float4 y = s_o[k][at];
+    const float f = ex2(ml.x - top);
+    l += ml.y * f;
+    a.x += y.x * f; a.y += y.y * f; a.z += y.z * f; a.w += y.w * f;
+  }
+  const float inv = l > 0.f ? 1.f / l : 0.f;
+  // place 8 k + g holds entries (kD / 8) g + 4 k ..
+  T* dst = out + b * P.os[0] + j * P.os[1] + mm * P.os[2] + (kD / 8) * (at & 7) + 4 * (at >> 3);
+  a.x *= inv; a.y *= inv; a.z *= inv; a.w *= inv;
+  if (sizeof(T) == 2) {
+    const __nv_bfloat162 lo = __floats2bfloat162_rn(a.x, a.y), hi = __floats2bfloat162_rn(a.z, a.w);
+    *reinterpret_cast<uint2*>(dst) = make_uint2(*reinterpret_cast<const uint32_t*>(&lo), *reinterpret_cast<const uint32_t*>(&hi));
+  } else {
+    *reinterpret_cast<float4*>(dst) = a;
+  }
+  if (at == 0) P.lse2[(long long)unit * P.live + r1] = l > 0.f ? top + log2f(l) : INFINITY;
+  if (at == 0 && lse != nullptr)
+    lse[((long long)b * P.Hq + j) * P.rows + mm] = l > 0.f ? (top + log2f(l)) * 0.693147180559945309f : -INFINITY;
+}
+
+// weight_out = weight_in + the sum of 2^(logit - log-sum-exp) over the rows: four tokens of a head per thread.
+__global__ void __launch_bounds__(kJoinThreads)
+attend_weight_kernel(const __grid_constant__ AttendParams P, const int32_t* __restrict__ row_counts, const float* weight_in, float* weight_out) {
+  __shared__ float s_lse[kMaxRows];
+  grid_dependency_wait();
+  const Cache& c = P.c;
+  const int tid = threadIdx.x, unit = blockIdx.y;
+  const long long len = c.length(unit), tok0 = (long long)blockIdx.x * kJoinTokens + tid;
+  if (tok0 - tid >= len) return;
+  const int rows = row_count(P, row_counts, unit / c.Hkv);
+  const float* logits = P.logits + ((long long)unit * P.row_tiles * c.cap + tok0) * P.logit_rows;
+  float2 x0[kJoinEach][2];                             // the first rows' logits
+  float w[kJoinEach];
+#pragma unroll
+  for (int k = 0; k < kJoinEach; ++k) {
+    const long long tok = tok0 + k * kJoinThreads;
+    w[k] = 0.f;
+    x0[k][0] = x0[k][1] = make_float2(0.f, 0.f);
+    if (tok < len) {
+      if (weight_in != nullptr) w[k] = weight_in[(long long)unit * c.cap + tok];
+      const float* y = logits + (long long)k * kJoinThreads * P.logit_rows;
+      x0[k][0] = *reinterpret_cast<const float2*>(y);
+      if (P.logit_rows > 2) x0[k][1] = *reinterpret_cast<const float2*>(y + 2);
+    }
+  }
+  // (infinity weighs nothing: rows that are not there, or see no token)
+  if (tid < kMaxRows) s_lse[tid] = tid < P.live && (P.row0 + tid) % P.rows < rows ? P.lse2[(long long)unit * P.live + tid] : INFINITY;
+  __syncthreads();
+#pragma unroll
+  for (int k = 0; k < kJoinEach; ++k) {
+    const long long tok = tok0 + k * kJoinThreads;
+    if (tok >= len) continue;
+    float sum = ex2(x0[k][0].x - s_lse[0]) + ex2(x0[k][0].y - s_lse[1]);
+    if (P.logit_rows > 2) sum += ex2(x0[k][1].x - s_lse[2]) + ex2(x0[k][1].y - s_lse[3]);
     for (int rt = 0; rt < P.row_tiles; ++rt) {
-      const float* s = P.logits + (((long long)unit * P.row_tiles + rt) * c.cap + tok) * P.logit_rows;
+      const float* y = logits + ((long long)rt * c.cap + (long long)k * kJoinThreads) * P.logit_rows;
       const int n = min(P.live - rt * P.tile_rows, P.tile_rows);
-      for (int i = 0; i < n; i += 2) {
-        const float2 x = *reinterpret_cast<const float2*>(s + i);
-        w += ex2(x.x - s_lse[rt * P.tile_rows + i]);
-        if (i + 1 < n) w += ex2(x.y - s_lse[rt * P.tile_rows + i + 1]);
+      for (int i = rt == 0 ? 4 : 0; i < n; i += 2) {
+        const float2 v = *reinterpret_cast<const float2*>(y + i);
+        sum += ex2(v.x - s_lse[rt * P.tile_rows + i]);
+        if (i + 1 < n) sum += ex2(v.y - s_lse[rt * P.tile_rows + i + 1]);
       }
     }
-    const long long i = (long long)unit * c.cap + tok;
-    weight_out[i] = (weight_in == nullptr ? 0.f : weight_in[i]) + w;
+    weight_out[(long long)unit * c.cap + tok] = w[k] + sum;
   }
 }
 
@@ -828,7 +855,7 @@ int tile_rows_of(int live, int dtype) { return live <= 8 ? 8 : live <= 16 || dty
 
 struct AttendLayout {
   int live, tile_rows, row_tiles, logit_rows;
-  size_t o, ml, before, logits, total;
+  size_t o, ml, before, lse2, logits, total;
 };
 
 AttendLayout attend_layout(const AttendParams& P, int dtype, bool with_weight) {
@@ -843,7 +870,8 @@ AttendLayout attend_layout(const AttendParams& P, int dtype, bool with_weight) {
   y.o = 0;
   y.ml = align_up(slots * y.tile_rows * P.c.d * sizeof(float));
   y.before = y.ml + align_up(slots * y.tile_rows * sizeof(float2));
-  y.logits = y.before + align_up(((size_t)P.c.units() + 1) * sizeof(long long));
+  y.lse2 = y.before + align_up(((size_t)P.c.units() + 1) * sizeof(long long));
+  y.logits = y.lse2 + align_up((size_t)P.c.units() * kMaxRows * sizeof(float));
   y.total = y.logits + (with_weight ? align_up((size_t)P.c.units() * y.row_tiles * P.c.cap * y.logit_rows * sizeof(float)) : 0);
   return y;
 }
@@ -887,12 +915,17 @@ kvc_status run_attend(AttendParams& P, const AttendLayout& y, const T* q, const 
     else
       s = e4m3 ? launch_split_form<T, KVC_E4M3, 64>(P, weight, q, row_counts, st) : launch_split_form<T, KVC_INT8, 64>(P, weight, q, row_counts, st);
     if (s != KVC_OK) return s;
-    const long long chunks = weight ? (P.c.cap + kJoinTokens - 1) / kJoinTokens : 0;
-    const long long ctas = P.c.units() * (P.live + chunks);
-    KVC_REQUIRE8(ctas < (1LL << 31), KVC_ERR_UNSUPPORTED, "batch * n_kv_heads * capacity is too large");
-    KVC_CUDA(launch_dependent(P.c.d == 128 ? attend_join_kernel<T, 128> : attend_join_kernel<T, 64>, dim3((unsigned)ctas), dim3(kJoinThreads),
-                              0, st, P, row_counts, out, lse, weight_in, weight_out, (int)chunks));
+    // a CTA per row while that keeps the GPU busy; many heads, whose parts are few: several rows in a CTA
+    int shift = 0;
+    while (shift < 3 && (P.live >> shift) > 1 && (long long)P.c.units() * ((P.live + (1 << shift) - 1) >> shift) > 2LL * P.ctas) ++shift;
+    KVC_CUDA(launch_dependent(P.c.d == 128 ? attend_join_kernel<T, 128> : attend_join_kernel<T, 64>,
+                              dim3((unsigned)P.c.units() * ((P.live + (1 << shift) - 1) >> shift)), dim3(kJoinThreads), 0, st, P, row_counts,
+                              out, lse, shift));
     KVC_LAUNCH_CHECK("attend_join_kernel");
+    if (!weight) continue;
+    KVC_CUDA(launch_dependent(attend_weight_kernel, dim3((unsigned)((P.c.cap + kJoinTokens - 1) / kJoinTokens), P.c.units()), dim3(kJoinThreads),
+                              0, st, P, row_counts, weight_in, weight_out));
+    KVC_LAUNCH_CHECK("attend_weight_kernel");
     weight_in = weight_out;                          // (later rows add to what the first ones gave)
   }
   return KVC_OK;
@@ -934,6 +967,7 @@ kvc_status kvc_attend(const kvc_cache* cache, const kvc_attend_desc* desc, const
   P.part_o = (float*)((char*)workspace + y.o);
   P.part_ml = (float2*)((char*)workspace + y.ml);
   P.before = (long long*)((char*)workspace + y.before);
+  P.lse2 = (float*)((char*)workspace + y.lse2);
   P.logits = (float*)((char*)workspace + y.logits);
   return desc->dtype == KVC_F32 ? run_attend<float>(P, y, (const float*)q, row_counts, (float*)out, lse, weight_in, weight_out, (cudaStream_t)stream)
                                 : run_attend<__nv_bfloat16>(P, y, (const __nv_bfloat16*)q, row_counts, (__nv_bfloat16*)out, lse, weight_in,
