@@ -49,7 +49,7 @@ struct AttendParams {
   float scale;
   long long qs[3], os[3];
   // of this launch: query rows row0 .. row0 + live - 1 of the G * rows of a KV head, in row_tiles tiles of 8 * kTiles
-  int row0, live, row_tiles, tile_rows, ctas, warps, logit_rows;
+  int row0, live, row_tiles, tile_rows, ctas, warps, logit_rows, device;
   float* part_o;                          // [slot][tile_rows][d]
   float2* part_ml;                        // [slot][tile_rows]: largest logit (in powers of two), sum of 2^(logit - it)
   float* logits;                          // [unit][row tile][token][logit_rows]
@@ -882,7 +882,8 @@ kvc_status launch_split(AttendParams& P, const T* q, const int32_t* row_counts, 
   static_assert(F::kWarps <= kMaxWarps && F::kSmem <= 220 * 1024, "shared memory and slots");
   auto kernel = attend_split_kernel<T, kFormat, kD, kTiles, kWeight>;
   P.warps = F::kWarps;
-  KVC_CUDA(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, F::kSmem));
+  static std::atomic<uint64_t> done{0};
+  KVC_CUDA(allow_smem(kernel, F::kSmem, done, P.device));
   KVC_CUDA(launch_dependent(kernel, dim3(P.ctas), dim3(F::kThreads), F::kSmem, st, P, q, row_counts));
   KVC_LAUNCH_CHECK("attend_split_kernel");
   return KVC_OK;
@@ -963,6 +964,7 @@ kvc_status kvc_attend(const kvc_cache* cache, const kvc_attend_desc* desc, const
   KVC_CUDA(cudaGetDevice(&dev));
   KVC_CUDA(cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev));
   P.ctas = sms < kMaxCtas ? sms : kMaxCtas;
+  P.device = dev;
   P.tile_rows = y.tile_rows; P.logit_rows = y.logit_rows;
   P.part_o = (float*)((char*)workspace + y.o);
   P.part_ml = (float2*)((char*)workspace + y.ml);

@@ -227,6 +227,8 @@ struct ReadParams {
   long long rows;
 };
 
+constexpr int kReadEach = 4;             // pieces of 16 codes per thread, asked for together
+
 template <typename T, int kFormat>
 __global__ void __launch_bounds__(256)
 cache_read_kernel(const __grid_constant__ ReadParams P, const int32_t* __restrict__ first, T* __restrict__ k_out, T* __restrict__ v_out) {
@@ -240,33 +242,43 @@ cache_read_kernel(const __grid_constant__ ReadParams P, const int32_t* __restric
   const int8_t* exps = (is_v ? c.v_exp : c.k_exp) + (long long)unit * c.blocks;
   T* out = (is_v ? v_out : k_out) + unit * P.rows * c.d;
   const long long total = P.rows << shift;
-  for (long long i = (long long)blockIdx.x * blockDim.x + threadIdx.x; i < total; i += (long long)gridDim.x * blockDim.x) {
-    const long long r = row_first + (i >> shift);
-    const int col = (int)(i & ((1 << shift) - 1)) * 16;
-    uint4 w = make_uint4(0, 0, 0, 0);
-    float f = 0.f;
-    if (r >= 0 && r < len) {
-      w = ld16_stream(codes + r * c.st[2] + col);
-      f = pow2_clamped(exps[r >> c.block_shift]);
-    }
-    float x[16];
-    decode4<kFormat>(w.x, x); decode4<kFormat>(w.y, x + 4); decode4<kFormat>(w.z, x + 8); decode4<kFormat>(w.w, x + 12);
-    T* o = out + (i << 4);
-    if (sizeof(T) == 2) {
-      uint32_t u[8];
+  for (long long i0 = (long long)blockIdx.x * (256 * kReadEach) + threadIdx.x; i0 < total; i0 += (long long)gridDim.x * (256 * kReadEach)) {
+    uint4 w[kReadEach];
+    float f[kReadEach];
 #pragma unroll
-      for (int q = 0; q < 8; ++q) {
-        const __nv_bfloat162 t = __floats2bfloat162_rn(x[2 * q] * f, x[2 * q + 1] * f);
-        u[q] = *reinterpret_cast<const uint32_t*>(&t);
+    for (int u = 0; u < kReadEach; ++u) {
+      const long long i = i0 + 256 * u, r = row_first + (i >> shift);
+      w[u] = make_uint4(0, 0, 0, 0);
+      f[u] = 0.f;
+      if (i < total && r >= 0 && r < len) {
+        w[u] = ld16_stream(codes + r * c.st[2] + (int)(i & ((1 << shift) - 1)) * 16);
+        f[u] = pow2_clamped(exps[r >> c.block_shift]);
       }
-      st32(o, u);
-    } else {
+    }
 #pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        uint32_t u[8];
+    for (int u = 0; u < kReadEach; ++u) {
+      const long long i = i0 + 256 * u;
+      if (i >= total) break;
+      T* o = out + (i << 4);
+      const uint32_t v[4] = {w[u].x, w[u].y, w[u].z, w[u].w};
 #pragma unroll
-        for (int q = 0; q < 8; ++q) u[q] = __float_as_uint(x[8 * h + q] * f);
-        st32(reinterpret_cast<char*>(o) + 32 * h, u);
+      for (int h = 0; h < (int)sizeof(T) / 2; ++h) {        // 32 bytes of output at a time
+        constexpr int kWords = 8 / (int)sizeof(T);          // of codes
+        uint32_t y[8];
+#pragma unroll
+        for (int q = 0; q < kWords; ++q) {
+          float x[4];
+          decode4<kFormat>(v[kWords * h + q], x);
+          if (sizeof(T) == 2) {
+            const __nv_bfloat162 s = __floats2bfloat162_rn(x[0] * f[u], x[1] * f[u]), t = __floats2bfloat162_rn(x[2] * f[u], x[3] * f[u]);
+            y[2 * q] = *reinterpret_cast<const uint32_t*>(&s);
+            y[2 * q + 1] = *reinterpret_cast<const uint32_t*>(&t);
+          } else {
+#pragma unroll
+            for (int z = 0; z < 4; ++z) y[(4 * q + z) & 7] = __float_as_uint(x[z] * f[u]);
+          }
+        }
+        st32(reinterpret_cast<char*>(o) + 32 * h, y);
       }
     }
   }
@@ -428,7 +440,7 @@ kvc_status kvc_cache_read(const kvc_cache* cache, const int32_t* first, int64_t 
   if ((s = require_device()) != KVC_OK) return s;
   P.rows = rows;
   const long long items = rows * P.c.d / 16;
-  long long ctas = (items + 255) / 256;
+  long long ctas = (items + 256 * kReadEach - 1) / (256 * kReadEach);
   if (ctas > 65536) ctas = 65536;
   const dim3 grid((unsigned)ctas, P.c.units(), k_out != nullptr && v_out != nullptr ? 2 : 1);
   const bool e4m3 = P.c.format == KVC_E4M3;

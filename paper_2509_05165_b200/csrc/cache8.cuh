@@ -3,6 +3,8 @@
 
 #include <cuda_fp8.h>
 
+#include <atomic>
+
 #include "kvc_internal.cuh"
 
 namespace kvc {
@@ -218,6 +220,16 @@ __device__ __forceinline__ void load8(const T* p, float* x) {
   Raw8<T> r;
   r.load(p);
   r.values(x);
+}
+
+// cudaFuncSetAttribute's opt-in to more shared memory, once per kernel and device (`done`: a word of the call site's own).
+template <typename Kernel>
+inline cudaError_t allow_smem(Kernel kernel, int bytes, std::atomic<uint64_t>& done, int dev) {
+  const uint64_t bit = 1ull << (dev & 63);
+  if ((done.load(std::memory_order_relaxed) & bit) != 0) return cudaSuccess;
+  const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+  if (e == cudaSuccess && dev < 64) done.fetch_or(bit, std::memory_order_relaxed);
+  return e;
 }
 
 // Threads of a CTA that works on blocks: at least 256, and whole jobs.

@@ -317,7 +317,8 @@ extern "C" kvc_status kvc_evict(const kvc_cache* src, const kvc_cache* dst, cons
   KVC_CUDA(cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev));
   const int ctas = select_ctas(a.cap, U, sms);
   const long long each = ((a.cap + 4 * ctas - 1) / (4 * ctas)) * 4;
-  KVC_CUDA(cudaFuncSetAttribute(evict_select_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSelKeep * 4));
+  static std::atomic<uint64_t> done{0};
+  KVC_CUDA(allow_smem(evict_select_kernel, kSelKeep * 4, done, dev));
   cudaLaunchAttribute attr[2];
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr[0].val.programmaticStreamSerializationAllowed = 1;

@@ -140,7 +140,7 @@ class Cache:
         self.batch, self.n_kv_heads, self.capacity, self.head_dim, self.format = b, h, cap, d, fmt
         self.struct = KvcCache(b, h, d, block, fmt, 0, cap, ks, k.data_ptr(), v.data_ptr(), k_exp.data_ptr(), v_exp.data_ptr(),
                                lengths.data_ptr())
-        self.ref, self.plans = C.byref(self.struct), _Plans()
+        self.ref, self.plans, self.device = C.byref(self.struct), _Plans(), dev
 
     @property
     def bytes(self) -> int:
@@ -220,21 +220,24 @@ def kvc_cache_gather(desc, k: Sequence[torch.Tensor], v: Sequence[torch.Tensor],
                      device_status: Optional[torch.Tensor] = None, stream=None) -> None:
     """``kvc_gather`` into 8-bit caches, one per layer.  idx [L, batch, Hkv, N] int32 or None; n_keep [batch, L] (or, with
     ``per_head``, [batch, L, Hkv]) int32 or None.  device_status: int32, becomes KVC_ERR_CAPACITY if rows did not fit."""
-    L, b, h, n = desc.n_layers, desc.batch, desc.n_kv_heads, desc.n_ctx
+    L, b, h, n, d = desc.n_layers, desc.batch, desc.n_kv_heads, desc.n_ctx, desc.head_dim
     _refuse(not (len(k) == len(v) == len(caches) == L), "k, v and caches hold one entry per layer (%d)", L)
     dtype = torch.float32 if desc.dtype == F32 else torch.bfloat16
-    _rows4(k[0], "k or v", b, h, n, desc.head_dim, dtype)
-    given = list(desc.kv_stride) if desc.kv_stride[0] else [h * n * desc.head_dim, n * desc.head_dim, desc.head_dim]
-    _refuse(any(k[0].shape[i] > 1 and k[0].stride(i) != given[i] for i in range(3)), "k or v has other strides than desc.kv_stride")
-    like = _sig(k[0])
+    given = tuple(desc.kv_stride) if desc.kv_stride[0] else (h * n * d, n * d, d)
+    like = None
     for t in (*k, *v):
-        if _sig(t) != like:             # (another stride of a dimension of one is none)
-            _rows4(t, "k or v", b, h, n, desc.head_dim, dtype)
+        sig = _sig(t)
+        if sig != like:
+            _rows4(t, "k or v", b, h, n, d, dtype)
             _refuse(any(t.shape[i] > 1 and t.stride(i) != given[i] for i in range(3)), "k or v has other strides than desc.kv_stride")
+            _refuse(like is not None and sig[3] != like[3], "tensors on different devices")
+            like = sig
     _dense(idx, "idx", torch.int32, L, b, h, n)
     _dense(n_keep, "n_keep", torch.int32, *((b, L, h) if per_head else (b, L)))
     _refuse(device_status is not None and device_status.dtype != torch.int32, "device_status must be int32")
-    dev = _one_device(k[0], *k, *v, idx, n_keep, device_status, *(c.k for c in caches))
+    dev = _one_device(k[0], idx, n_keep, device_status)
+    for c in caches:
+        _refuse(c.device != dev, "tensors on different devices")
     structs = (KvcCache * L)(*(c.struct for c in caches))
     _check(_load().kvc_cache_gather(C.byref(desc), _ptr_array(k), _ptr_array(v), _ptr(idx), _ptr(n_keep), int(per_head), structs,
                                     _ptr(device_status), _launch_stream(dev, stream)))
