@@ -23,7 +23,7 @@
 // to block: P goes in relative to 2^M, M a running maximum of logit + exponent, which keeps the largest terms of a row at
 // full precision whatever block they are in, and 2^5 times larger, so that 2^17 weights of 2^-26 are not lost beside one of
 // 1/2, as they are in an fp16 of at most 1.  References only move when they are exceeded by 2^10 (2^60 for the sums): until
-// then no lane needs another's maximum (with a maximum per step, four rows over 128K tokens 79 -> XX us).
+// then no lane needs another's maximum (with a maximum per step, four rows over 128K tokens took 79 us instead of 68).
 #include <math.h>
 
 #include "cache8.cuh"
@@ -33,7 +33,8 @@ namespace {
 
 constexpr int kGranule = 64;              // tokens: unit of the split
 constexpr int kSetup = 2;                 // granules that a head's start counts as
-constexpr int kMaxWarps = 12;
+constexpr int kAttWarps = 8;              // (12 with fewer registers each: 32 ragged sequences 51 -> 53 us, four rows over 128K tokens in two
+                                          // tiles of 16 64 -> 77)
 constexpr int kMaxCtas = 256;             // bounds the workspace, whatever the device
 constexpr int kMaxRows = 64;              // query rows of a KV head that one launch takes (bounds the logits kept)
 constexpr float kSlackSum = 60.f;         // logits may exceed the reference of the sums by this much (see Form for V's)
@@ -54,7 +55,7 @@ struct AttendParams {
   float2* part_ml;                        // [slot][tile_rows]: largest logit (in powers of two), sum of 2^(logit - it)
   float* logits;                          // [unit][row tile][token][logit_rows]
   float* lse2;                            // [unit][live]
-  long long* before;                      // [units + 1]: granules (with kSetup) in front of a head, per row tile; all of them last
+  int* before;                            // [units + 1]: granules (with kSetup) in front of a head, per row tile; all of them last
 };
 
 __device__ __forceinline__ float ex2(float x) {
@@ -118,24 +119,19 @@ __device__ __forceinline__ long long tokens_seen(const AttendParams& P, int rr, 
 // Granules of a head's row tile, what starting it costs included.
 __device__ __forceinline__ int granules(long long len) { return len == 0 ? 0 : (int)((len + kGranule - 1) / kGranule) + kSetup; }
 
-// a / b of non-negative numbers; nearly always 32-bit ones, whose division takes a fraction of the time.
-__device__ __forceinline__ long long quotient(long long a, long long b) {
-  return ((a | b) >> 32) == 0 ? (long long)((uint32_t)a / (uint32_t)b) : a / b;
-}
-
-// `total` granules cut into `parts` shares, as many of them as there are granules at most: share i, and the share of a place.
-// The first `more` shares hold one granule more than the others.
+// `total` granules (of all heads and row tiles: under 2^31, see resolve_attend) cut into `parts` shares, as many of them as there are
+// granules at most: share i, and the share of a place.  The first `more` shares hold one granule more than the others.
 struct Shares {
-  long long each;
-  int parts, more;
-  __device__ __forceinline__ Shares(long long total, int parts_) : parts(total < parts_ ? (int)total : parts_) {
-    each = quotient(total, parts);
-    more = (int)(total - each * parts);
+  uint32_t each, more;
+  int parts;
+  __device__ __forceinline__ Shares(int total, int parts_) : parts(min(total, parts_)) {
+    each = (uint32_t)total / (uint32_t)parts;
+    more = (uint32_t)total - each * parts;
   }
-  __device__ __forceinline__ long long begin(int i) const { return each * i + min(i, more); }
-  __device__ __forceinline__ int of(long long place) const {
-    const long long larger = more * (each + 1);
-    return place < larger ? (int)quotient(place, each + 1) : more + (int)quotient(place - larger, each);
+  __device__ __forceinline__ int begin(int i) const { return (int)(each * i + min((uint32_t)i, more)); }
+  __device__ __forceinline__ int of(int place) const {
+    const uint32_t larger = more * (each + 1);
+    return (uint32_t)place < larger ? (uint32_t)place / (each + 1) : more + ((uint32_t)place - larger) / each;
   }
 };
 
@@ -147,7 +143,7 @@ struct Form {
   // 2^-29 of the row's largest weight (fp32: 2^-36, at the price of references that move more often)
   static constexpr float kLift = kTwo ? 12.f : 5.f, kSlack = kTwo ? 3.f : 10.f;
   static constexpr bool kQShared = kTiles == 4;        // Q's operands in shared memory (else in registers)
-  static constexpr int kWarps = kTiles == 1 ? 12 : kTiles == 2 && !kTwo ? 10 : 8;
+  static constexpr int kWarps = kAttWarps;
   static constexpr int kThreads = kWarps * 32;
   static constexpr int kSteps = kD / 16;               // k steps of Q K^T, and row tiles of V^T
   static constexpr int kKPieces = kD / 64;             // 16-byte pieces of a token's K per lane
@@ -170,9 +166,8 @@ attend_split_kernel(const __grid_constant__ AttendParams P, const T* __restrict_
   constexpr bool kTwo = F::kTwo;
   constexpr int kWarps = F::kWarps, kThreads = F::kThreads, kSteps = F::kSteps, kStages = F::kStages, kRows = F::kRows, kPitch = F::kPitch;
   extern __shared__ __align__(128) char smem[];
-  __shared__ long long s_sum[kWarps];
-  __shared__ int s_unit[kWarps + 1];                   // the head that each warp's piece starts in; last: the whole share's
-  __shared__ long long s_before[kWarps + 1];
+  __shared__ int s_sum[kWarps];
+  __shared__ int s_unit[kWarps + 1], s_before[kWarps + 1];      // the head that each warp's piece starts in; last: the whole share's
   __shared__ float s_stat[kWarps][kRows][2];
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t = lane & 3;
   grid_dependency_wait();
@@ -182,24 +177,25 @@ attend_split_kernel(const __grid_constant__ AttendParams P, const T* __restrict_
   // ---- this CTA's share, and the heads that it and its warps' pieces start in
   const int per = (units + kThreads - 1) / kThreads;
   const int u0 = tid * per, u1 = min(u0 + per, units);
-  long long mine = 0;
+  int mine = 0;
   for (int u = u0; u < u1; ++u) mine += granules(c.length(u));
-  long long incl = mine;
+  int incl = mine;
 #pragma unroll
   for (int o = 1; o < 32; o <<= 1) {
-    const long long y = __shfl_up_sync(0xffffffffu, incl, o);
+    const int y = __shfl_up_sync(0xffffffffu, incl, o);
     if (lane >= o) incl += y;
   }
   if (lane == 31) s_sum[warp] = incl;
   __syncthreads();
-  long long total = 0;
+  int total = 0;
 #pragma unroll
   for (int w = 0; w < kWarps; ++w) {
-    if (w < warp) incl += s_sum[w];
-    total += s_sum[w];
+    const int y = s_sum[w];
+    if (w < warp) incl += y;
+    total += y;
   }
   if (blockIdx.x == 0) {                               // for attend_join_kernel
-    long long b = incl - mine;
+    int b = incl - mine;
     for (int u = u0; u < u1; ++u) {
       P.before[u] = b;
       b += granules(c.length(u));
@@ -210,47 +206,43 @@ attend_split_kernel(const __grid_constant__ AttendParams P, const T* __restrict_
   if (total == 0) return;
   const Shares ctas(total, P.ctas);
   if ((int)blockIdx.x >= ctas.parts) return;
-  const long long share0 = ctas.begin(blockIdx.x), share1 = ctas.begin(blockIdx.x + 1);
-  const Shares pieces(share1 - share0, kWarps);
-  if (mine > 0) {
-    long long v = (incl - mine) * P.row_tiles;
-    if (v < share1 && incl * P.row_tiles > share0) {
-      for (int u = u0; u < u1; ++u) {
-        const long long n = (long long)granules(c.length(u)) * P.row_tiles;
-        if (v <= share0 && share0 < v + n) { s_unit[kWarps] = u; s_before[kWarps] = v; }
-        for (int w = 0; w < pieces.parts; ++w) {
-          const long long p = share0 + pieces.begin(w);
-          if (v <= p && p < v + n) { s_unit[w] = u; s_before[w] = v; }
-        }
-        v += n;
+  const int share0 = ctas.begin(blockIdx.x), share1 = ctas.begin(blockIdx.x + 1);
+  // the head that holds place p: found by the thread that has it
+  auto find = [&](int p, int which) {
+    int v = (incl - mine) * P.row_tiles;
+    if (v > p || p >= incl * P.row_tiles) return;
+    for (int u = u0;; ++u) {
+      const int n = granules(c.length(u)) * P.row_tiles;
+      if (p < v + n) {
+        s_unit[which] = u;
+        s_before[which] = v;
+        return;
       }
+      v += n;
     }
-  }
+  };
+  find(share0, kWarps);
   __syncthreads();
-  // within one row tile of one head: all warps work on it together
-  bool together;
-  long long at, end, before;                           // the place, its end, where the row tile begins
-  int unit, n_gran, rt;
-  long long len;
-  {
-    unit = s_unit[kWarps];
-    before = s_before[kWarps];
-    n_gran = granules(c.length(unit));
-    if (P.row_tiles > 1) before += quotient(share0 - before, n_gran) * n_gran;
-    together = share1 <= before + n_gran;
-    at = share0;
-    end = share1;
-    if (!together) {
-      if (warp >= pieces.parts) return;                // (no barrier follows for a CTA of several heads)
-      at = share0 + pieces.begin(warp);
-      end = share0 + pieces.begin(warp + 1);
-      unit = s_unit[warp];
-      before = s_before[warp];
-    }
-    len = c.length(unit);
+  int at = share0, end = share1;                       // the place, and its end
+  int unit = s_unit[kWarps], before = s_before[kWarps];        // .. and where the row tile begins that it lies in
+  int len = (int)c.length(unit), n_gran = granules(len);
+  int rt = P.row_tiles > 1 ? (at - before) / n_gran : 0;
+  before += rt * n_gran;
+  // within one row tile of one head: all warps work on it together; else each on a piece of its own
+  const bool together = share1 <= before + n_gran;
+  if (!together) {
+    const Shares pieces(share1 - share0, kWarps);
+    for (int w = 0; w < pieces.parts; ++w) find(share0 + pieces.begin(w), w);
+    __syncthreads();
+    if (warp >= pieces.parts) return;                  // (no barrier follows for a CTA of several heads)
+    at = share0 + pieces.begin(warp);
+    end = share0 + pieces.begin(warp + 1);
+    unit = s_unit[warp];
+    before = s_before[warp];
+    len = (int)c.length(unit);
     n_gran = granules(len);
-    rt = P.row_tiles > 1 ? (int)quotient(at - (together ? s_before[kWarps] : before), n_gran) : 0;
-    before = (together ? s_before[kWarps] : before) + (long long)rt * n_gran;
+    rt = P.row_tiles > 1 ? (at - before) / n_gran : 0;
+    before += rt * n_gran;
   }
   const int warp_in = together ? warp : 0, warps_in = together ? kWarps : 1;
   const int st = (int)c.st[2];                         // (a row's stride; 31 bits, checked by the host)
@@ -261,9 +253,9 @@ attend_split_kernel(const __grid_constant__ AttendParams P, const T* __restrict_
   while (true) {
     // ---- a part of one row tile of one head: tokens [lo, hi)
     const int b = unit / c.Hkv, h = unit - b * c.Hkv;
-    const long long upto = min(end, before + n_gran);
-    const int lo = max((int)(at - before) - kSetup, 0) * kGranule;
-    const int hi = min((long long)max((int)(upto - before) - kSetup, 0) * kGranule, len);
+    const int upto = min(end, before + n_gran);
+    const int lo = max(at - before - kSetup, 0) * kGranule;
+    const int hi = (int)min((long long)max(upto - before - kSetup, 0) * kGranule, (long long)len);
     const int rows = row_count(P, row_counts, b);
     const int first_row = P.row0 + rt * kRows, last_row = min(P.row0 + P.live, first_row + kRows);
     const int live_rows = last_row - first_row;
@@ -278,42 +270,41 @@ attend_split_kernel(const __grid_constant__ AttendParams P, const T* __restrict_
     const uint8_t* vp = c.v + c.base(unit) + (long long)(first + 2 * t) * st + F::kVBytes * g;
     const long long advance = (long long)stride * st;
 
-    auto fetch = [&](int it) {                         // step `it` into stage it % kStages
+    // K, and V, of step `it` into stage it % kStages, each a group of copies.  Rows behind the end are filled with zeros.
+    auto fetch_k = [&](int it) {
       if (it < iters) {
         const uint32_t dst = my_smem_addr + (it % kStages) * F::kStageBytes;
         const int left = hi - first - it * stride;     // tokens from this step on
-        if (left >= 32) {
 #pragma unroll
-          for (int i = 0; i < 4; ++i)
+        for (int i = 0; i < 4; ++i) {
+          const bool live = left >= 32 || 8 * i + g < left;
+          const uint8_t* src = live ? kp + (long long)(8 * i) * st : c.k;
 #pragma unroll
-            for (int p = 0; p < F::kKPieces; ++p)
-              copy_async<16>(dst + ((i * F::kKPieces + p) * 32 + lane) * 16, kp + (long long)(8 * i) * st + 64 * p, true);
-#pragma unroll
-          for (int i = 0; i < 8; ++i)
-            copy_async<F::kVBytes>(dst + F::kVBase + (i * 32 + lane) * F::kVBytes,
-                                   vp + (long long)(16 * (i >> 2) + 8 * ((i >> 1) & 1) + (i & 1)) * st, true);
-        } else {                                       // rows behind the end are filled with zeros, their addresses not used
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const bool live = 8 * i + g < left;
-#pragma unroll
-            for (int p = 0; p < F::kKPieces; ++p)
-              copy_async<16>(dst + ((i * F::kKPieces + p) * 32 + lane) * 16, live ? kp + (long long)(8 * i) * st + 64 * p : c.k, live);
-          }
-#pragma unroll
-          for (int i = 0; i < 8; ++i) {
-            const int tok = 16 * (i >> 2) + 8 * ((i >> 1) & 1) + (i & 1);
-            const bool live = tok + 2 * t < left;
-            copy_async<F::kVBytes>(dst + F::kVBase + (i * 32 + lane) * F::kVBytes, live ? vp + (long long)tok * st : c.v, live);
-          }
+          for (int p = 0; p < F::kKPieces; ++p) copy_async<16>(dst + ((i * F::kKPieces + p) * 32 + lane) * 16, src + (live ? 64 * p : 0), live);
         }
         kp += advance;
+      }
+      copy_commit();
+    };
+    auto fetch_v = [&](int it) {
+      if (it < iters) {
+        const uint32_t dst = my_smem_addr + (it % kStages) * F::kStageBytes + F::kVBase;
+        const int left = hi - first - it * stride;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          const int tok = 16 * (i >> 2) + 8 * ((i >> 1) & 1) + (i & 1);
+          const bool live = left >= 32 || tok + 2 * t < left;
+          copy_async<F::kVBytes>(dst + (i * 32 + lane) * F::kVBytes, live ? vp + (long long)tok * st : c.v, live);
+        }
         vp += advance;
       }
       copy_commit();
     };
 #pragma unroll
-    for (int s = 0; s < kStages - 1; ++s) fetch(s);
+    for (int s = 0; s < kStages; ++s) {
+      fetch_k(s);
+      fetch_v(s);
+    }
 
     // exponents of the two halves of 32 tokens, K's and V's: a lane reads those of one step in 32, four bytes in one register
     uint32_t exps = 0;
@@ -400,8 +391,7 @@ attend_split_kernel(const __grid_constant__ AttendParams P, const T* __restrict_
       if (it > 0 && (it & 31) == 0) fetch_exps(it);
       const uint32_t four = __shfl_sync(0xffffffffu, exps, it & 31);
       const int ek[2] = {(int8_t)four, (int8_t)(four >> 8)}, ev[2] = {(int8_t)(four >> 16), (int8_t)(four >> 24)};
-      fetch(it + kStages - 1);
-      copy_wait<kStages - 1>();
+      copy_wait<2 * kStages - 1>();                    // K of this step is there; behind it, V and kStages - 1 steps more
       const char* stage = my_smem + (it % kStages) * F::kStageBytes;
       const int tok0 = first + it * stride;
 
@@ -446,6 +436,7 @@ attend_split_kernel(const __grid_constant__ AttendParams P, const T* __restrict_
           }
         }
       }
+      fetch_k(it + kStages);                           // (into the place just read)
 #pragma unroll
       for (int f = 0; f < 2; ++f) {
         const float kf = pow2_clamped(ek[f]);
@@ -517,6 +508,7 @@ attend_split_kernel(const __grid_constant__ AttendParams P, const T* __restrict_
       }
 
       // ---- P, and its share of the outputs
+      copy_wait<2 * kStages - 1>();                    // V of this step is there
 #pragma unroll
       for (int f = 0; f < 2; ++f) {
         uint32_t ph[kTiles][2], pl[kTwo ? kTiles : 1][2];
@@ -577,6 +569,7 @@ attend_split_kernel(const __grid_constant__ AttendParams P, const T* __restrict_
           }
         }
       }
+      fetch_v(it + kStages);
     }
     copy_wait<0>();
 #pragma unroll
@@ -660,7 +653,7 @@ attend_split_kernel(const __grid_constant__ AttendParams P, const T* __restrict_
     before += n_gran;
     if (++rt == P.row_tiles) {
       rt = 0;
-      do len = c.length(++unit); while (len == 0);     // (one is left: at < end <= total)
+      do len = (int)c.length(++unit); while (len == 0);     // (one is left: at < end <= total)
       n_gran = granules(len);
     }
   }
@@ -668,35 +661,34 @@ attend_split_kernel(const __grid_constant__ AttendParams P, const T* __restrict_
 
 // The parts of a row tile: up to three runs of slots, of the warps of its first CTA, of whole CTAs, of the warps of its last.
 struct Parts {
-  long long slot[3];
-  int n[3], step1;                                     // the middle run's slots lie step1 apart
+  int slot[3], n[3], step1;                            // the middle run's slots lie step1 apart
   __device__ __forceinline__ int count() const { return n[0] + n[1] + n[2]; }
   __device__ __forceinline__ long long operator[](int i) const {
-    return i < n[0] ? slot[0] + i : i < n[0] + n[1] ? slot[1] + (long long)(i - n[0]) * step1 : slot[2] + (i - n[0] - n[1]);
+    return i < n[0] ? slot[0] + i : i < n[0] + n[1] ? slot[1] + (i - n[0]) * step1 : slot[2] + (i - n[0] - n[1]);
   }
 };
 
 __device__ __forceinline__ Parts parts_of(const AttendParams& P, int unit, int rt) {
   Parts r{};
   r.step1 = P.warps;
-  const long long b = P.before[unit], n = P.before[unit + 1] - b;
+  const int b = P.before[unit], n = P.before[unit + 1] - b, total = P.before[P.c.units()];
   if (n == 0) return r;
-  const Shares ctas(P.before[P.c.units()] * P.row_tiles, P.ctas);
-  const long long u = (long long)unit * P.row_tiles + rt, v0 = b * P.row_tiles + rt * n, v1 = v0 + n;
+  const Shares ctas(total * P.row_tiles, P.ctas);
+  const int u = unit * P.row_tiles + rt, v0 = b * P.row_tiles + rt * n, v1 = v0 + n;
   const int c0 = ctas.of(v0 + kSetup), c1 = ctas.of(v1 - 1);
   int mid0 = c0, mid1 = c1;                            // CTAs that lie wholly inside
+#pragma unroll
   for (int side = 0; side < 2; ++side) {
     const int cta = side == 0 ? c0 : c1;
-    const long long s0 = ctas.begin(cta), s1 = ctas.begin(cta + 1);
+    const int s0 = ctas.begin(cta), s1 = ctas.begin(cta + 1);
     if ((side == 1 && c1 == c0) || (v0 <= s0 && s1 <= v1)) continue;
     const Shares pieces(s1 - s0, P.warps);
-    const long long from = max(v0 + kSetup, s0) - s0, to = min(v1, s1) - s0;
-    const int w0 = pieces.of(from), w1 = pieces.of(to - 1);
-    r.slot[side == 0 ? 0 : 2] = (long long)cta * P.warps + w0 + u;
-    r.n[side == 0 ? 0 : 2] = w1 - w0 + 1;
+    const int w0 = pieces.of(max(v0 + kSetup, s0) - s0), w1 = pieces.of(min(v1, s1) - s0 - 1);
+    r.slot[2 * side] = cta * P.warps + w0 + u;
+    r.n[2 * side] = w1 - w0 + 1;
     if (side == 0) mid0 = c0 + 1; else mid1 = c1 - 1;
   }
-  r.slot[1] = (long long)mid0 * P.warps + u;
+  r.slot[1] = mid0 * P.warps + u;
   r.n[1] = max(mid1 - mid0 + 1, 0);
   return r;
 }
@@ -843,6 +835,9 @@ kvc_status resolve_attend(const kvc_cache* cache, const kvc_attend_desc* d, Atte
   KVC_REQUIRE8(d->reserved_ == 0, KVC_ERR_INVALID_ARG, "reserved_ must be 0");
   KVC_REQUIRE8(isfinite(d->scale), KVC_ERR_INVALID_ARG, "scale is not finite");
   KVC_REQUIRE8(P->c.st[2] < (1LL << 31), KVC_ERR_UNSUPPORTED, "tokens of the cache lie 2^31 bytes or more apart");
+  // (places in the granules of all heads and row tiles are 32-bit numbers)
+  KVC_REQUIRE8((long long)P->c.units() * (P->c.cap / kGranule + 1 + kSetup) * (kMaxRows / 8) < (1LL << 31), KVC_ERR_UNSUPPORTED,
+               "batch * n_kv_heads * capacity must be below 2^34");
   P->Hq = d->n_q_heads; P->G = d->n_q_heads / P->c.Hkv; P->rows = d->rows; P->causal = d->causal;
   P->scale = d->scale > 0.f ? d->scale : 1.0f / sqrtf((float)P->c.d);
   const int eb = d->dtype == KVC_F32 ? 4 : 2;
@@ -866,11 +861,11 @@ AttendLayout attend_layout(const AttendParams& P, int dtype, bool with_weight) {
   y.row_tiles = (y.live + y.tile_rows - 1) / y.tile_rows;
   y.logit_rows = 2;
   while (y.logit_rows < y.live && y.logit_rows < y.tile_rows) y.logit_rows *= 2;
-  const size_t slots = (size_t)kMaxCtas * kMaxWarps + (size_t)P.c.units() * y.row_tiles;
+  const size_t slots = (size_t)kMaxCtas * kAttWarps + (size_t)P.c.units() * y.row_tiles;
   y.o = 0;
   y.ml = align_up(slots * y.tile_rows * P.c.d * sizeof(float));
   y.before = y.ml + align_up(slots * y.tile_rows * sizeof(float2));
-  y.lse2 = y.before + align_up(((size_t)P.c.units() + 1) * sizeof(long long));
+  y.lse2 = y.before + align_up(((size_t)P.c.units() + 1) * sizeof(int));
   y.logits = y.lse2 + align_up((size_t)P.c.units() * kMaxRows * sizeof(float));
   y.total = y.logits + (with_weight ? align_up((size_t)P.c.units() * y.row_tiles * P.c.cap * y.logit_rows * sizeof(float)) : 0);
   return y;
@@ -879,7 +874,7 @@ AttendLayout attend_layout(const AttendParams& P, int dtype, bool with_weight) {
 template <typename T, int kFormat, int kD, int kTiles, bool kWeight>
 kvc_status launch_split(AttendParams& P, const T* q, const int32_t* row_counts, cudaStream_t st) {
   using F = Form<T, kD, kTiles>;
-  static_assert(F::kWarps <= kMaxWarps && F::kSmem <= 220 * 1024, "shared memory and slots");
+  static_assert(F::kSmem <= 220 * 1024, "shared memory and slots");
   auto kernel = attend_split_kernel<T, kFormat, kD, kTiles, kWeight>;
   P.warps = F::kWarps;
   static std::atomic<uint64_t> done{0};
@@ -968,7 +963,7 @@ kvc_status kvc_attend(const kvc_cache* cache, const kvc_attend_desc* desc, const
   P.tile_rows = y.tile_rows; P.logit_rows = y.logit_rows;
   P.part_o = (float*)((char*)workspace + y.o);
   P.part_ml = (float2*)((char*)workspace + y.ml);
-  P.before = (long long*)((char*)workspace + y.before);
+  P.before = (int*)((char*)workspace + y.before);
   P.lse2 = (float*)((char*)workspace + y.lse2);
   P.logits = (float*)((char*)workspace + y.logits);
   return desc->dtype == KVC_F32 ? run_attend<float>(P, y, (const float*)q, row_counts, (float*)out, lse, weight_in, weight_out, (cudaStream_t)stream)
