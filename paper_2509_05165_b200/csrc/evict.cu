@@ -305,6 +305,7 @@ extern "C" kvc_status kvc_evict(const kvc_cache* src, const kvc_cache* dst, cons
   const long long sa = span(a), sb = span(b), U = a.units();
   KVC_REQUIRE8(!overlap(a.k, sa, b.k, sb) && !overlap(a.k, sa, b.v, sb) && !overlap(a.v, sa, b.k, sb) && !overlap(a.v, sa, b.v, sb) &&
                    !overlap(a.k_exp, U * a.blocks, b.k_exp, U * b.blocks) && !overlap(a.v_exp, U * a.blocks, b.v_exp, U * b.blocks) &&
+                   !overlap(a.k_exp, U * a.blocks, b.v_exp, U * b.blocks) && !overlap(a.v_exp, U * a.blocks, b.k_exp, U * b.blocks) &&
                    !overlap(a.lengths, 4 * U, b.lengths, 4 * U),
                KVC_ERR_INVALID_ARG, "src and dst share memory");
   KVC_REQUIRE8(weight_out == nullptr || !overlap(weight, 4 * U * a.cap, weight_out, 4 * U * b.cap), KVC_ERR_INVALID_ARG,

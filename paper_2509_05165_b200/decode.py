@@ -88,6 +88,8 @@ _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
 def _launch_stream(dev: int, stream):
     """The stream to launch on; the tensors' device has to be the current one (launches go there)."""
     if dev < 0:
+        # (host memory: without a GPU the library says what else is wrong, and that there is none; with one it must not see it)
+        _refuse(torch.cuda.is_available(), "tensors in host memory")
         return _stream(stream)
     if dev != _get_device():
         raise KvcError(-1, "tensors on cuda:%d, which is not the current device" % dev)

@@ -461,6 +461,104 @@ def test_evict(dev, fmt, d, sb, db, cap, budget, recent):
             assert torch.equal(_bits(dst.v)[i, j, m:], left[i, j, m:])
 
 
+# ---- what the calls allow beyond the ordinary --------------------------------------------------------------------------
+
+def test_host_tensors_are_refused_beside_a_gpu(dev):
+    c = kvc.alloc_cache(1, 1, 64, 20, 16, I8, "cpu")
+    q = torch.zeros((1, 1, 1, 64), dtype=BF)
+    ws = torch.zeros(kvc.kvc_attend_workspace_size(c, q, False) + 256, dtype=torch.uint8)
+    for call in (lambda: kvc.kvc_attend(c, q, q.clone(), workspace=ws[-ws.data_ptr() % 256:]), lambda: kvc.kvc_cache_append(c, q, q),
+                 lambda: kvc.kvc_cache_read(c, q, None), lambda: kvc.kvc_rotary(kvc.Rotary(64), q, None, torch.zeros(1, dtype=torch.int64)),
+                 lambda: kvc.kvc_attend(kvc.alloc_cache(1, 1, 64, 20, 16, I8, dev), q.to(dev), q, workspace=ws.to(dev))):
+        with pytest.raises(kvc.KvcError) as e:
+            call()
+        assert e.value.status == -1
+
+
+def test_gather_into_caches_of_different_capacities(dev):
+    """Layers keep different numbers of rows, so their caches differ; with and without room to spare."""
+    L, h, d, n = 3, 2, 64, 260
+    g = _gen(21)
+    k, v = [[torch.randn((1, h, n, d), generator=g).to(BF).to(dev) for _ in range(L)] for _ in range(2)]
+    keep = torch.tensor([[7, 260, 129]], dtype=torch.int32)
+    caches = [_poisoned(1, h, d, cap, 32, E4, dev) for cap in (7, 300, 130)]
+    desc = kvc.kvc_desc_init(L, 1, h, h, d, n, 1, kvc.BF16)
+    status = torch.zeros(1, dtype=torch.int32, device=dev)
+    kvc.kvc_cache_gather(desc, k, v, None, keep.to(dev), caches, device_status=status)
+    assert int(status) == 0
+    for l, c in enumerate(caches):
+        m = int(keep[0, l])
+        assert (c.lengths == m).all()
+        for x, src in zip(R.cache_values(c), (k, v)):
+            for j in range(h):
+                assert torch.equal(x[0, j, :m], R.Held(E4, 32).fill(src[l][0, j, :m].cpu()).values())
+
+
+@pytest.mark.parametrize("fmt", [I8, E4])
+def test_heads_inside_tokens_and_offsets_beyond_32_bits(dev, fmt):
+    """A cache whose second sequence, or whose tokens, lie gigabytes apart, and rows as a projection leaves them: the same as a
+    dense one, code by code and bit by bit."""
+    g = _gen(31)
+    b, h, d, cap, rows = 2, 2, 64, 70, 40
+    k_new, v_new = [R.spread_rows(g, b, rows, h, d).to(BF).to(dev).transpose(1, 2) for _ in range(2)]
+    q = torch.randn((b, 3, 2 * h, d), generator=g).to(BF).to(dev).transpose(1, 2)
+    big = 2 ** 32 + 2 ** 20
+    for stride in ((big, d, h * d, 1), (d * h, d, big // 64 // 16 * 16, 1)):
+        span = sum((s - 1) * t for s, t in zip((b, h, cap), stride)) + d
+        stores = [torch.empty(span, dtype=torch.uint8, device=dev) for _ in range(2)]
+        views = [s.view(fmt).as_strided((b, h, cap, d), stride) for s in stores]
+        dense = kvc.alloc_cache(b, h, d, cap, 16, fmt, dev)
+        far = kvc.Cache(*views, torch.zeros_like(dense.k_exp), torch.zeros_like(dense.v_exp), torch.zeros_like(dense.lengths), 16)
+        outs = []
+        for c in (dense, far):
+            kvc.kvc_cache_append(c, k_new, v_new)
+            kvc.kvc_cache_append(c, k_new[:, :, :25], v_new[:, :, :25])
+            out, lse = torch.empty_like(q), torch.empty((b, 2 * h, 3), device=dev)
+            weight = torch.zeros((b, h, cap), device=dev)
+            ws = torch.empty(kvc.kvc_attend_workspace_size(c, q, True), dtype=torch.uint8, device=dev)
+            kvc.kvc_attend(c, q, out, lse, weight=weight, workspace=ws)
+            ko, vo = [torch.empty((b, h, cap, d), dtype=F32, device=dev) for _ in range(2)]
+            kvc.kvc_cache_read(c, ko, vo)
+            small = kvc.alloc_cache(b, h, d, 30, 32, fmt, dev)
+            idx = torch.empty((b, h, 30), dtype=torch.int32, device=dev)
+            kvc.kvc_evict(c, small, weight, 30, 8, idx)
+            outs.append([c.lengths, c.k_exp, c.v_exp, out, lse, weight, ko, vo, idx, _bits(small.k), small.v_exp])
+        assert all(torch.equal(x, y) for x, y in zip(*outs))
+        assert (outs[0][0] == 65).all()
+        want = torch.cat([R.Held(fmt, 16).append(k_new[1, 1].cpu()).append(k_new[1, 1, :25].cpu()).values(), torch.zeros((5, d))])
+        assert torch.equal(outs[0][6][1, 1].cpu().double(), want)
+        del stores, views, far, outs
+        torch.cuda.empty_cache()
+
+
+def test_many_query_heads_and_rows_of_one_head(dev):
+    """More query rows of a KV head than one launch takes, with weights; and the same call captured twice over one workspace."""
+    g = _gen(41)
+    lengths = torch.tensor([[333], [50]])
+    c = _filled_cache(dev, g, 2, 1, 64, 340, 64, I8, lengths)
+    q = torch.randn((2, 128, 2, 64), generator=g).to(BF).to(dev)
+    out, lse = torch.empty_like(q), torch.empty((2, 128, 2), device=dev)
+    w0 = torch.rand((2, 1, 340), generator=g).to(dev)
+    weight = torch.full_like(w0, -9.0)
+    ws = torch.empty(kvc.kvc_attend_workspace_size(c, q, True), dtype=torch.uint8, device=dev)
+    kvc.kvc_attend(c, q, out, lse, weight=w0, weight_out=weight, workspace=ws)
+    _check_attend(c, q, out, lse, weight, w0, True, 1 / 8.0)
+    few, small = q[:, :2].contiguous(), torch.empty_like(q[:, :2])
+    graphs = [torch.cuda.CUDAGraph() for _ in range(2)]
+    with torch.cuda.graph(graphs[0]):
+        kvc.kvc_attend(c, q, out, workspace=ws)
+    with torch.cuda.graph(graphs[1]):
+        kvc.kvc_attend(c, few, small, workspace=ws)
+    want, want_small = out.clone(), torch.empty_like(small)
+    kvc.kvc_attend(c, few, want_small, workspace=ws)
+    for _ in range(3):
+        out.zero_()
+        small.zero_()
+        graphs[0].replay()
+        graphs[1].replay()
+        assert torch.equal(out, want) and torch.equal(small, want_small)
+
+
 # ---- together ----------------------------------------------------------------------------------------------------------
 
 @pytest.mark.parametrize("fmt,dtype", [(E4, BF), (I8, F32)])
