@@ -217,32 +217,34 @@ def kvc_rotary(rope: Rotary, q: Optional[torch.Tensor], k: Optional[torch.Tensor
                               _launch_stream(plan[2], stream)))
 
 
+_gather_plans = _Plans()
+
+
+def _gather_plan(desc, k, v, idx, n_keep, caches, per_head, device_status):
+    L, b, h, n, d = desc.n_layers, desc.batch, desc.n_kv_heads, desc.n_ctx, desc.head_dim
+    _refuse(not (len(k) == len(v) == len(caches) == L), "k, v and caches hold one entry per layer (%d)", L)
+    dtype = torch.float32 if desc.dtype == F32 else torch.bfloat16
+    given = tuple(desc.kv_stride) if desc.kv_stride[0] else (h * n * d, n * d, d)
+    for t in (*k, *v):
+        _rows4(t, "k or v", b, h, n, d, dtype)
+        _refuse(any(t.shape[i] > 1 and t.stride(i) != given[i] for i in range(3)), "k or v has other strides than desc.kv_stride")
+    _dense(idx, "idx", torch.int32, L, b, h, n)
+    _dense(n_keep, "n_keep", torch.int32, *((b, L, h) if per_head else (b, L)))
+    _refuse(device_status is not None and device_status.dtype != torch.int32, "device_status must be int32")
+    return (_one_device(k[0], *k, *v, idx, n_keep, device_status, *(c.k for c in caches)),)
+
+
 def kvc_cache_gather(desc, k: Sequence[torch.Tensor], v: Sequence[torch.Tensor], idx: Optional[torch.Tensor],
                      n_keep: Optional[torch.Tensor], caches: Sequence[Cache], per_head: bool = False,
                      device_status: Optional[torch.Tensor] = None, stream=None) -> None:
     """``kvc_gather`` into 8-bit caches, one per layer.  idx [L, batch, Hkv, N] int32 or None; n_keep [batch, L] (or, with
     ``per_head``, [batch, L, Hkv]) int32 or None.  device_status: int32, becomes KVC_ERR_CAPACITY if rows did not fit."""
-    L, b, h, n, d = desc.n_layers, desc.batch, desc.n_kv_heads, desc.n_ctx, desc.head_dim
-    _refuse(not (len(k) == len(v) == len(caches) == L), "k, v and caches hold one entry per layer (%d)", L)
-    dtype = torch.float32 if desc.dtype == F32 else torch.bfloat16
-    given = tuple(desc.kv_stride) if desc.kv_stride[0] else (h * n * d, n * d, d)
-    like = None
-    for t in (*k, *v):
-        sig = _sig(t)
-        if sig != like:
-            _rows4(t, "k or v", b, h, n, d, dtype)
-            _refuse(any(t.shape[i] > 1 and t.stride(i) != given[i] for i in range(3)), "k or v has other strides than desc.kv_stride")
-            _refuse(like is not None and sig[3] != like[3], "tensors on different devices")
-            like = sig
-    _dense(idx, "idx", torch.int32, L, b, h, n)
-    _dense(n_keep, "n_keep", torch.int32, *((b, L, h) if per_head else (b, L)))
-    _refuse(device_status is not None and device_status.dtype != torch.int32, "device_status must be int32")
-    dev = _one_device(k[0], idx, n_keep, device_status)
-    for c in caches:
-        _refuse(c.device != dev, "tensors on different devices")
-    structs = (KvcCache * L)(*(c.struct for c in caches))
+    key = (bytes(desc), per_head, tuple(map(_sig, k)), tuple(map(_sig, v)), _sig(idx), _sig(n_keep), _sig(device_status),
+           tuple([c.device for c in caches]))
+    plan = _gather_plans.get(key) or _gather_plans.keep(key, _gather_plan(desc, k, v, idx, n_keep, caches, per_head, device_status))
+    structs = (KvcCache * len(caches))(*[c.struct for c in caches])
     _check(_load().kvc_cache_gather(C.byref(desc), _ptr_array(k), _ptr_array(v), _ptr(idx), _ptr(n_keep), int(per_head), structs,
-                                    _ptr(device_status), _launch_stream(dev, stream)))
+                                    _ptr(device_status), _launch_stream(plan[0], stream)))
 
 
 def _append_plan(cache, k_new, v_new, n_new, lengths_out, weight, device_status):
