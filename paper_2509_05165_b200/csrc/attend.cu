@@ -146,6 +146,7 @@ struct Form {
   static constexpr float kLift = kTwo ? 12.f : 5.f, kSlack = kTwo ? 3.f : 10.f;
   static constexpr bool kQShared = kTiles == 4;        // Q's operands in shared memory (else in registers)
   static constexpr int kWarps = kAttWarps;
+  static constexpr int kHalves = kTiles == 4 ? 1 : 2;  // a step's 32 tokens at once, or 16 by 16 (four tiles: the registers)
   static constexpr int kThreads = kWarps * 32;
   static constexpr int kSteps = kD / 16;               // k steps of Q K^T, and row tiles of V^T
   static constexpr int kKPieces = kD / 64;             // 16-byte pieces of a token's K per lane
@@ -166,7 +167,7 @@ __global__ void __launch_bounds__(Form<T, kD, kTiles>::kThreads, 1)
 attend_split_kernel(const __grid_constant__ AttendParams P, const T* __restrict__ q, const int32_t* __restrict__ row_counts) {
   using F = Form<T, kD, kTiles>;
   constexpr bool kTwo = F::kTwo;
-  constexpr int kWarps = F::kWarps, kThreads = F::kThreads, kSteps = F::kSteps, kStages = F::kStages, kRows = F::kRows, kPitch = F::kPitch;
+  constexpr int kWarps = F::kWarps, kThreads = F::kThreads, kSteps = F::kSteps, kStages = F::kStages, kRows = F::kRows, kPitch = F::kPitch, kH = F::kHalves;
   extern __shared__ __align__(128) char smem[];
   __shared__ int s_sum[kWarps];
   __shared__ int s_unit[kWarps + 1], s_before[kWarps + 1];      // the head that each warp's piece starts in; last: the whole share's
@@ -392,32 +393,35 @@ attend_split_kernel(const __grid_constant__ AttendParams P, const T* __restrict_
     for (int it = 0; it < iters; ++it) {
       if (it > 0 && (it & 31) == 0) fetch_exps(it);
       const uint32_t four = __shfl_sync(0xffffffffu, exps, it & 31);
-      const int ek[2] = {(int8_t)four, (int8_t)(four >> 8)}, ev[2] = {(int8_t)(four >> 16), (int8_t)(four >> 24)};
       copy_wait<2 * kStages - 1>();                    // K of this step is there; behind it, V and kStages - 1 steps more
       const char* stage = my_smem + (it % kStages) * F::kStageBytes;
-      const int tok0 = first + it * stride;
+#pragma unroll 1
+      for (int half = 0; half < 2; half += kH) {       // kH times 16 tokens at once
+      const uint32_t mine = half == 0 ? four : four >> 8;
+      const int ek[2] = {(int8_t)mine, (int8_t)(mine >> 8)}, ev[2] = {(int8_t)(mine >> 16), (int8_t)(mine >> 24)};
+      const int tok0 = first + it * stride + 16 * half;
 
       // ---- logits, in powers of two: lane holds tokens g and g + 8 (of each 16), columns 2 t and 2 t + 1
-      float sc[2][kTiles][4];
+      float sc[kH][kTiles][4];
 #pragma unroll
-      for (int f = 0; f < 2; ++f)
+      for (int f = 0; f < kH; ++f)
 #pragma unroll
         for (int n = 0; n < kTiles; ++n)
 #pragma unroll
           for (int i = 0; i < 4; ++i) sc[f][n][i] = 0.f;
 #pragma unroll
       for (int p = 0; p < F::kKPieces; ++p) {
-        uint32_t x[4][4];
+        uint32_t x[2 * kH][4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const uint4 w = *reinterpret_cast<const uint4*>(stage + ((i * F::kKPieces + p) * 32 + lane) * 16);
+        for (int i = 0; i < 2 * kH; ++i) {
+          const uint4 w = *reinterpret_cast<const uint4*>(stage + (((2 * half + i) * F::kKPieces + p) * 32 + lane) * 16);
           x[i][0] = w.x; x[i][1] = w.y; x[i][2] = w.z; x[i][3] = w.w;
         }
 #pragma unroll
         for (int s = 0; s < 4; ++s) {
-          uint32_t a[2][4];
+          uint32_t a[kH][4];
 #pragma unroll
-          for (int f = 0; f < 2; ++f) {
+          for (int f = 0; f < kH; ++f) {
             to_half2<kFormat>(x[2 * f][s], &a[f][0], &a[f][2]);
             to_half2<kFormat>(x[2 * f + 1][s], &a[f][1], &a[f][3]);
           }
@@ -431,25 +435,25 @@ attend_split_kernel(const __grid_constant__ AttendParams P, const T* __restrict_
               b0 = qh[n][4 * p + s][0]; b1 = qh[n][4 * p + s][1];
             }
 #pragma unroll
-            for (int f = 0; f < 2; ++f) {
+            for (int f = 0; f < kH; ++f) {
               mma16816(sc[f][n], a[f], b0, b1);
               if (kTwo) mma16816(sc[f][n], a[f], ql[n][4 * p + s][0], ql[n][4 * p + s][1]);
             }
           }
         }
       }
-      fetch_k(it + kStages);                           // (into the place just read)
+      if (half + kH == 2) fetch_k(it + kStages);       // (into the place just read)
 #pragma unroll
-      for (int f = 0; f < 2; ++f) {
+      for (int f = 0; f < kH; ++f) {
         const float kf = pow2_clamped(ek[f]);
 #pragma unroll
         for (int n = 0; n < kTiles; ++n)
 #pragma unroll
           for (int i = 0; i < 4; ++i) sc[f][n][i] *= factor[n][i & 1] * kf;
       }
-      if (tok0 + 32 > seen_least) {
+      if (tok0 + 16 * kH > seen_least) {
 #pragma unroll
-        for (int f = 0; f < 2; ++f)
+        for (int f = 0; f < kH; ++f)
 #pragma unroll
           for (int n = 0; n < kTiles; ++n)
 #pragma unroll
@@ -458,7 +462,7 @@ attend_split_kernel(const __grid_constant__ AttendParams P, const T* __restrict_
       }
       if (kWeight) {
 #pragma unroll
-        for (int f = 0; f < 2; ++f)
+        for (int f = 0; f < kH; ++f)
 #pragma unroll
           for (int i = 0; i < 2; ++i) {
             const int tok = tok0 + 16 * f + 8 * i + g;
@@ -474,22 +478,32 @@ attend_split_kernel(const __grid_constant__ AttendParams P, const T* __restrict_
       // ---- references of the logits and of logit + V's exponent.  They move when a lane finds one exceeded by more than the slack:
       // then to the maxima of these tokens over all lanes, and sums and outputs follow.
       const float evf[2] = {(float)ev[0], (float)ev[1]};
+      auto tops = [&](int n, int i, float* ms, float* mv) {      // of the lane's tokens
+        *ms = fmaxf(sc[0][n][i], sc[0][n][2 + i]);
+        *mv = *ms + evf[0];
+        if (kH == 2) {
+          const float m1 = fmaxf(sc[kH - 1][n][i], sc[kH - 1][n][2 + i]);
+          *ms = fmaxf(*ms, m1);
+          *mv = fmaxf(*mv, m1 + evf[1]);
+        }
+      };
       float over = -INFINITY;
 #pragma unroll
       for (int n = 0; n < kTiles; ++n)
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
-          const float m0 = fmaxf(sc[0][n][i], sc[0][n][2 + i]), m1 = fmaxf(sc[1][n][i], sc[1][n][2 + i]);
-          over = fmaxf(over, fmaxf(m0 + evf[0], m1 + evf[1]) - top_v[n][i] - F::kSlack);
-          over = fmaxf(over, fmaxf(m0, m1) - top_s[n][i] - kSlackSum);
+          float ms, mv;
+          tops(n, i, &ms, &mv);
+          over = fmaxf(over, mv - top_v[n][i] - F::kSlack);
+          over = fmaxf(over, ms - top_s[n][i] - kSlackSum);
         }
       if (__any_sync(0xffffffffu, over > 0.f)) {
 #pragma unroll
         for (int n = 0; n < kTiles; ++n)
 #pragma unroll
           for (int i = 0; i < 2; ++i) {
-            const float m0 = fmaxf(sc[0][n][i], sc[0][n][2 + i]), m1 = fmaxf(sc[1][n][i], sc[1][n][2 + i]);
-            float ms = fmaxf(m0, m1), mv = fmaxf(m0 + evf[0], m1 + evf[1]);
+            float ms, mv;
+            tops(n, i, &ms, &mv);
 #pragma unroll
             for (int x = 4; x < 32; x <<= 1) {
               ms = fmaxf(ms, __shfl_xor_sync(0xffffffffu, ms, x));
@@ -510,9 +524,9 @@ attend_split_kernel(const __grid_constant__ AttendParams P, const T* __restrict_
       }
 
       // ---- P, and its share of the outputs
-      copy_wait<2 * kStages - 1>();                    // V of this step is there
+      copy_wait<2 * kStages - (kH == 2 ? 1 : 2)>();    // V of this step is there (K of a step more may have been asked for by now)
 #pragma unroll
-      for (int f = 0; f < 2; ++f) {
+      for (int f = 0; f < kH; ++f) {
         uint32_t ph[kTiles][2], pl[kTwo ? kTiles : 1][2];
 #pragma unroll
         for (int n = 0; n < kTiles; ++n) {
@@ -543,7 +557,7 @@ attend_split_kernel(const __grid_constant__ AttendParams P, const T* __restrict_
             }
           }
         }
-        const char* sv = stage + F::kVBase + (4 * f * 32 + lane) * F::kVBytes;
+        const char* sv = stage + F::kVBase + (4 * (half + f) * 32 + lane) * F::kVBytes;
         uint32_t v[4][F::kVBytes / 4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
@@ -570,6 +584,7 @@ attend_split_kernel(const __grid_constant__ AttendParams P, const T* __restrict_
             }
           }
         }
+      }
       }
       fetch_v(it + kStages);
     }
