@@ -11,8 +11,10 @@
 //   (kTiles of them share the converted codes).  Operand layouts: the order of the summed index is free as long as both
 //   operands agree, so lane (g, t) takes token g's entries 16 t .. 16 t + 15 of each 64 as its k slots, and entries (d / 8) g ..
 //   of its tokens of V as its rows; a transpose of P's 8 x 8 tiles (movmatrix) is the only exchange between lanes.  Legacy
-//   mma on purpose: an SM scheduler has 44 clocks per token before the codes arrive from HBM and mma takes 8 of them (8.0 clk
-//   per m16n8k16, measured); through tcgen05 the converted codes would have to go back to shared memory first.
+//   mma on purpose: while HBM brings a token's codes, the scheduler that will work on it has 44 clocks, and eight query rows take
+//   8 of them in mma (8.0 per m16n8k16, measured).  Through tcgen05 the converted codes have to go back to shared memory first and
+//   change hands between roles, 1.4 us per 128 tokens of waits alone: 109 us for the four rows over 128K tokens below, 41 for 32K
+//   tokens, in the form that was tried.
 // attend_join_kernel    joins the parts of a row (log-sum-exp).
 // attend_weight_kernel  adds the rows' weights from the logits, which the first kernel leaves in the workspace (they stay in L2; the
 //   softmax's denominator is known only after the last token).
@@ -24,6 +26,11 @@
 // full precision whatever block they are in, and 2^5 times larger, so that 2^17 weights of 2^-26 are not lost beside one of
 // 1/2, as they are in an fp16 of at most 1.  References only move when they are exceeded by 2^10 (2^60 for the sums): until
 // then no lane needs another's maximum (with a maximum per step, four rows over 128K tokens took 79 us instead of 68).
+//
+// B200: 8 sequences of 32768 tokens, 8 heads of 128, one row of 32 query heads 89 us (537 MB of codes, 6.0 TB/s); one such
+// sequence with weights 22.6 us, of which about 7 are the launches' own; four rows of 28 query heads over 131072 tokens of 4 heads
+// 54 us (2.5 TB/s): there the instructions bound it, 1200 per warp and 32 tokens with two warps per scheduler (the accumulators
+// fill the registers).
 #include <math.h>
 
 #include "cache8.cuh"

@@ -6,6 +6,8 @@
 // histogram of digits is fewer of them, but its atomics crowd into a few bins: 34 us for 64 heads of 32768 rows); the kept
 // positions are written in order.  evict_move_kernel, a job per block of the new cache (see cache8.cuh): kept rows are
 // read once, take the exponent of their new block and are written once.
+// B200: 256 heads from 2112 rows to 2048 selection 20 us, moving 48 us (268 MB, 5.6 TB/s); 64 heads of up to 32768 rows to 8192
+// selection 25 us, moving 18 us.
 #include "cache8.cuh"
 
 namespace kvc {

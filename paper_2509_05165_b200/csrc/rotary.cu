@@ -6,6 +6,8 @@
 // kRotUnroll heads' loads (32 bytes of a row each, 64 in fp32) in flight.
 // Angles: p f_i / 2pi in 64 bits, the whole turns taken off there (fp32 loses 0.008 rad at p = 131072, more than half a
 // step of bf16), the rest of a turn in fp32 through sincospif.
+// B200: 16001 tokens of 32 + 8 heads of 128 in bf16 62 us, 5.3 TB/s of reads and writes (a copy: 6.5); one token of 32
+// sequences 2.3 us, a launch.
 #include <math.h>
 
 #include "cache8.cuh"
@@ -14,8 +16,8 @@ namespace kvc {
 namespace {
 
 constexpr int kRotThreads = 256;
-constexpr int kRotRows = 16;                 // rows of a tile
-constexpr int kRotUnroll = 4;                // heads in flight
+constexpr int kRotRows = 8;                  // rows of a tile (16 with four heads in flight: 65 us instead of 62 for the prompt below)
+constexpr int kRotUnroll = 2;                // heads in flight
 
 struct RotaryParams {
   int Hq, Hkv, d, rows, rot, tile_shift, heads_per_cta;      // tiles of 2^tile_shift rows
