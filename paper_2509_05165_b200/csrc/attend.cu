@@ -531,7 +531,7 @@ attend_split_kernel(const __grid_constant__ AttendParams P, const T* __restrict_
       }
 
       // ---- P, and its share of the outputs
-      copy_wait<2 * kStages - (kH == 2 ? 1 : 2)>();    // V of this step is there (K of a step more may have been asked for by now)
+      if (half == 0) copy_wait<2 * kStages - (kH == 2 ? 1 : 2)>();      // V of this step is there (K of a step more has been asked for or not)
 #pragma unroll
       for (int f = 0; f < kH; ++f) {
         uint32_t ph[kTiles][2], pl[kTwo ? kTiles : 1][2];

@@ -225,10 +225,10 @@ __device__ __forceinline__ void load8(const T* p, float* x) {
 // cudaFuncSetAttribute's opt-in to more shared memory, once per kernel and device (`done`: a word of the call site's own).
 template <typename Kernel>
 inline cudaError_t allow_smem(Kernel kernel, int bytes, std::atomic<uint64_t>& done, int dev) {
-  const uint64_t bit = 1ull << (dev & 63);
+  const uint64_t bit = dev < 64 ? 1ull << dev : 0;
   if ((done.load(std::memory_order_relaxed) & bit) != 0) return cudaSuccess;
   const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
-  if (e == cudaSuccess && dev < 64) done.fetch_or(bit, std::memory_order_relaxed);
+  if (e == cudaSuccess) done.fetch_or(bit, std::memory_order_relaxed);
   return e;
 }
 

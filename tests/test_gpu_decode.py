@@ -559,6 +559,71 @@ def test_many_query_heads_and_rows_of_one_head(dev):
         assert torch.equal(out, want) and torch.equal(small, want_small)
 
 
+@pytest.mark.parametrize("rows", [1, 5])
+def test_more_heads_than_threads(dev, rows):
+    """1400 heads, most of them empty or of a few tokens, some long: every warp holds several of them; and their eviction."""
+    g = _gen(51 + rows)
+    b, h, d, cap = 700, 2, 64, 700
+    lengths = torch.randint(0, 40, (b, h), generator=g)
+    lengths[torch.rand((b, h), generator=g) < 0.4] = 0
+    lengths[::97, 1] = torch.randint(100, cap + 1, (len(lengths[::97]),), generator=g)
+    k, v = [torch.randint(-127, 128, (b, h, cap, d), generator=g).to(I8) for _ in range(2)]
+    ke, ve = [torch.randint(-9, -5, (b, h, -(-cap // 128)), generator=g).to(I8) for _ in range(2)]
+    c = kvc.Cache(k.to(dev), v.to(dev), ke.to(dev), ve.to(dev), lengths.to(torch.int32).to(dev), 128)
+    q = torch.randn((b, 3 * h, rows, d), generator=g).to(BF).to(dev)
+    out, lse = torch.empty_like(q), torch.empty((b, 3 * h, rows), device=dev)
+    w0 = torch.rand((b, h, cap), generator=g).to(dev)
+    weight = torch.full_like(w0, -9.0)
+    ws = torch.full((kvc.kvc_attend_workspace_size(c, q, True),), 0xFF, dtype=torch.uint8, device=dev)
+    kvc.kvc_attend(c, q, out, lse, weight=w0, weight_out=weight, workspace=ws)
+    _check_attend(c, q, out, lse, weight, w0, True, 1 / 8.0)
+    dst = kvc.alloc_cache(b, h, d, 20, 16, I8, dev)
+    idx = torch.empty((b, h, 20), dtype=torch.int32, device=dev)
+    kvc.kvc_evict(c, dst, weight, 20, 3, idx)
+    w, got = weight.cpu(), idx.cpu()
+    for i in range(b):
+        for j in range(h):
+            kept = R.evict(w[i, j], int(lengths[i, j]), 20, 3)
+            assert got[i, j].tolist() == kept + [-1] * (20 - len(kept))
+
+
+def test_calls_at_once_on_two_streams_and_captured_moves(dev):
+    """Calls that share nothing but the cache they read, in flight together; and append, eviction and reading in a graph."""
+    g = _gen(61)
+    c = _filled_cache(dev, g, 2, 2, 128, 6000, 64, E4, torch.tensor([[6000, 5000], [77, 0]]))
+    q = torch.randn((2, 8, 1, 128), generator=g).to(BF).to(dev)
+    w = torch.rand((2, 2, 6000), generator=g).to(dev)
+    ws = [torch.empty(kvc.kvc_attend_workspace_size(c, q, True), dtype=torch.uint8, device=dev) for _ in range(3)]
+    want, want_w = torch.empty_like(q), torch.full_like(w, -9.0)
+    kvc.kvc_attend(c, q, want, weight=w, weight_out=want_w, workspace=ws[2])
+    outs, sums = [torch.empty_like(q) for _ in range(2)], [torch.full_like(w, -9.0) for _ in range(2)]
+    streams = [torch.cuda.Stream(dev) for _ in range(2)]
+    torch.cuda.synchronize()
+    for _ in range(20):
+        for s, o, x, y in zip(streams, outs, sums, ws):
+            kvc.kvc_attend(c, q, o, weight=w, weight_out=x, workspace=y, stream=s)
+    torch.cuda.synchronize()
+    assert all(torch.equal(o, want) and torch.equal(x, want_w) for o, x in zip(outs, sums))
+    spare, idx = kvc.alloc_cache(2, 2, 128, 600, 32, E4, dev), torch.empty((2, 2, 500), dtype=torch.int32, device=dev)
+    k_new = torch.randn((2, 2, 9, 128), generator=g).to(BF).to(dev)
+    back = torch.empty((2, 2, 600, 128), dtype=BF, device=dev)
+
+    def moves():
+        kvc.kvc_evict(c, spare, w, 500, 100, idx)
+        kvc.kvc_cache_append(spare, k_new, k_new)
+        kvc.kvc_cache_read(spare, back, None)
+
+    moves()
+    plain = [t.clone() for t in (back, idx, spare.lengths, _bits(spare.v))]
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        moves()
+    for _ in range(2):
+        spare.k.view(torch.uint8).fill_(0x7F)
+        graph.replay()
+        assert all(torch.equal(x, y) for x, y in zip(plain[:3], (back, idx, spare.lengths)))
+
+
 # ---- together ----------------------------------------------------------------------------------------------------------
 
 @pytest.mark.parametrize("fmt,dtype", [(E4, BF), (I8, F32)])
