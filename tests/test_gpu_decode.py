@@ -461,6 +461,31 @@ def test_evict(dev, fmt, d, sb, db, cap, budget, recent):
             assert torch.equal(_bits(dst.v)[i, j, m:], left[i, j, m:])
 
 
+@pytest.mark.parametrize("n,budget,recent,h", [(60001, 20011, 333, 2), (350003, 9000, 0, 1), (350003, 340000, 200000, 1), (9000, 8999, 1, 3)])
+def test_evict_from_long_rows(dev, n, budget, recent, h):
+    """Rows shared by up to eight CTAs, and longer than these keep; ties over all of them, negative and infinite weights."""
+    g = _gen(n)
+    c = kvc.alloc_cache(1, h, 64, n + 3, 64, I8, dev)
+    c.k.random_(-100, 100)
+    c.lengths.fill_(n)
+    w = torch.randn((1, h, n + 3), generator=g).exp()
+    w[0, 0] = (w[0, 0] * 2).floor()                    # few values, many ties
+    if h > 1:
+        w[0, 1, ::5] *= -1.0
+        w[0, 1, 17], w[0, 1, 18] = math.inf, -math.inf
+    dst = kvc.alloc_cache(1, h, 64, budget, 64, I8, dev)
+    idx, wo = torch.empty((1, h, budget), dtype=torch.int32, device=dev), torch.empty((1, h, budget), device=dev)
+    kvc.kvc_evict(c, dst, w.to(dev), budget, recent, idx, wo)
+    free = n - recent
+    for j in range(h):
+        heavy = torch.sort(w[0, j, :free], descending=True, stable=True).indices[:budget - recent].sort().values
+        kept = torch.cat([heavy, torch.arange(free, n)])
+        assert torch.equal(idx[0, j].cpu().long(), kept) and torch.equal(wo[0, j].cpu(), w[0, j][kept])
+        a, b = c.k[0, j][kept.to(dev)].float() * torch.pow(2.0, c.k_exp[0, j][kept.to(dev) // 64].float())[:, None], None
+        b = dst.k[0, j].float() * torch.pow(2.0, dst.k_exp[0, j].float()).repeat_interleave(64)[:budget, None]
+        assert torch.equal(a, b)                       # (codes of up to 100 under one exponent keep their values)
+
+
 # ---- what the calls allow beyond the ordinary --------------------------------------------------------------------------
 
 def test_host_tensors_are_refused_beside_a_gpu(dev):
