@@ -35,31 +35,31 @@ cache_gather_kernel(const __grid_constant__ CacheGatherParams P, const int32_t* 
   grid_dependency_wait();
   const int l = blockIdx.z, unit = blockIdx.y, b = unit / P.Hkv, h = unit - b * P.Hkv;
   const GatherLayer& y = P.layer[l];
-  long long n = P.N;
+  long long kept = P.N;
   if (n_keep != nullptr) {
-    n = P.per_head ? n_keep[((long long)b * P.L + l) * P.Hkv + h] : n_keep[(long long)b * P.L + l];
-    n = n < 0 ? 0 : (n > P.N ? P.N : n);
+    kept = P.per_head ? n_keep[((long long)b * P.L + l) * P.Hkv + h] : n_keep[(long long)b * P.L + l];
+    kept = kept < 0 ? 0 : (kept > P.N ? P.N : kept);
   }
+  const int n = (int)min(kept, y.cap);                 // (capacities are below 2^31 - 1024)
   if (blockIdx.x == 0 && threadIdx.x == 0) {
-    y.lengths[unit] = (int32_t)(n < y.cap ? n : y.cap);
-    if (n > y.cap && device_status != nullptr) *device_status = KVC_ERR_CAPACITY;
+    y.lengths[unit] = n;
+    if (kept > n && device_status != nullptr) *device_status = KVC_ERR_CAPACITY;
   }
-  if (n > y.cap) n = y.cap;
 
   const JobLane<8> j(P.block_shift, P.d);
   const int slots = blockDim.x / j.threads;
   if (((long long)blockIdx.x * slots << P.block_shift) >= n) return;    // (the whole CTA)
-  const long long blk = (long long)blockIdx.x * slots + j.slot, row0 = blk << P.block_shift;
-  const long long from = b * P.kvs[0] + h * P.kvs[1];
+  const int blk = blockIdx.x * slots + j.slot, row0 = blk << P.block_shift;
+  const int left = n - row0 - j.row0;                  // of the thread's rows, those with g * row_step < left are there
+  const long long from = b * P.kvs[0] + h * P.kvs[1] + j.col;
   const T *ks = reinterpret_cast<const T*>(y.k) + from, *vs = reinterpret_cast<const T*>(y.v) + from;
-  const int32_t* map = idx == nullptr ? nullptr : idx + (((long long)l * P.Bt + b) * P.Hkv + h) * P.N;
-  long long at[4];
+  const int32_t* map = idx == nullptr ? nullptr : idx + (((long long)l * P.Bt + b) * P.Hkv + h) * P.N + row0 + j.row0;
+  int at[4];
 #pragma unroll
   for (int g = 0; g < 4; ++g) {
-    const long long r = row0 + j.row(g);
     at[g] = -1;
-    if (r < n) {
-      at[g] = map == nullptr ? r : map[r];
+    if (g * j.row_step < left) {
+      at[g] = map == nullptr ? row0 + j.row(g) : map[g * j.row_step];
       if (at[g] >= P.N) at[g] = -1;
     }
   }
@@ -67,8 +67,9 @@ cache_gather_kernel(const __grid_constant__ CacheGatherParams P, const int32_t* 
 #pragma unroll
   for (int g = 0; g < 4; ++g) {
     if (at[g] >= 0) {
-      kx[g].load(ks + at[g] * P.kvs[2] + j.col(g));
-      vx[g].load(vs + at[g] * P.kvs[2] + j.col(g));
+      const long long o = at[g] * P.kvs[2];
+      kx[g].load(ks + o);
+      vx[g].load(vs + o);
     } else {
       kx[g].zero();
       vx[g].zero();
@@ -83,13 +84,14 @@ cache_gather_kernel(const __grid_constant__ CacheGatherParams P, const int32_t* 
   const float2 top = job_max(make_float2(Raw8<T>::top(km), Raw8<T>::top(vm)), j, scratch);
   if (row0 >= n) return;
   const int ke = exponent_of<kFormat>(top.x), ve = exponent_of<kFormat>(top.y);
-  const long long to = b * y.st[0] + h * y.st[1];
+  const float kf = pow2(-ke), vf = pow2(-ve);
+  long long to = b * y.st[0] + h * y.st[1] + (row0 + j.row0) * y.st[2] + j.col;
+  const long long step = j.row_step * y.st[2];
 #pragma unroll
-  for (int g = 0; g < 4; ++g) {
-    const long long r = row0 + j.row(g), o = to + r * y.st[2] + j.col(g);
-    if (r < n) {
-      *reinterpret_cast<uint2*>(y.ko + o) = kx[g].template encode<kFormat>(pow2(-ke));
-      *reinterpret_cast<uint2*>(y.vo + o) = vx[g].template encode<kFormat>(pow2(-ve));
+  for (int g = 0; g < 4; ++g, to += step) {
+    if (g * j.row_step < left) {
+      *reinterpret_cast<uint2*>(y.ko + to) = kx[g].template encode<kFormat>(kf);
+      *reinterpret_cast<uint2*>(y.vo + to) = vx[g].template encode<kFormat>(vf);
     }
   }
   if (j.t == 0) {
@@ -155,10 +157,10 @@ cache_append_kernel(const __grid_constant__ AppendParams P, const T* __restrict_
     for (int g = 0; g < 4; ++g) {
       const int r = row0 + j.row(g) - len;                // the row's number among the new ones
       if (live && r >= 0 && r < n) {
-        const long long at = from + r * P.ns[2] + j.col(g);
+        const long long at = from + r * P.ns[2] + j.col;
         kx[g].load(k_new + at);
         vx[g].load(v_new + at);
-        if (weight != nullptr && j.col(g) == 0) weight[unit * c.cap + len + r] = 0.f;
+        if (weight != nullptr && j.col == 0) weight[unit * c.cap + len + r] = 0.f;
       } else {
         kx[g].zero();
         vx[g].zero();
@@ -185,7 +187,7 @@ cache_append_kernel(const __grid_constant__ AppendParams P, const T* __restrict_
 #pragma unroll
     for (int g = 0; g < 4; ++g) {
       const int r = row0 + j.row(g);
-      const long long o = to + r * c.st[2] + j.col(g);
+      const long long o = to + r * c.st[2] + j.col;
       if (r >= len && r < len + n) {
         *reinterpret_cast<uint2*>(c.k + o) = kx[g].template encode<kFormat>(pow2(-ke));
         *reinterpret_cast<uint2*>(c.v + o) = vx[g].template encode<kFormat>(pow2(-ve));

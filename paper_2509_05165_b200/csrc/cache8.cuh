@@ -120,18 +120,22 @@ __device__ __forceinline__ float max_value(uint32_t pairs) {
 
 // A block's tokens as one job of block * d / 32 threads with 32 values of K and of V each, in groups of kGroup values of a row.
 // The jobs of a CTA lie side by side; a job is one warp or whole warps.
+// A job's threads are a multiple of a row's groups, so a thread has the same place in each of its rows.
 template <int kGroup>
 struct JobLane {
   static constexpr int kGroups = 32 / kGroup;
-  int threads, slot, t, per_row_shift;    // per_row_shift: log2(d / kGroup)
+  int threads, slot, t, row0, row_step, col;           // rows row0, row0 + row_step, ..; entries from col on
   __device__ __forceinline__ JobLane(int block_shift, int d) {
-    per_row_shift = (d == 128 ? 7 : 6) - (kGroup == 8 ? 3 : 4);
-    threads = 1 << (block_shift + (d == 128 ? 2 : 1));
-    slot = threadIdx.x / threads;
-    t = threadIdx.x - slot * threads;
+    const int per_row_shift = (d == 128 ? 7 : 6) - (kGroup == 8 ? 3 : 4);      // log2(d / kGroup)
+    const int shift = block_shift + (d == 128 ? 2 : 1);
+    threads = 1 << shift;
+    slot = threadIdx.x >> shift;
+    t = threadIdx.x & (threads - 1);
+    row0 = t >> per_row_shift;
+    row_step = threads >> per_row_shift;
+    col = (t & ((1 << per_row_shift) - 1)) * kGroup;
   }
-  __device__ __forceinline__ int row(int g) const { return (g * threads + t) >> per_row_shift; }
-  __device__ __forceinline__ int col(int g) const { return ((g * threads + t) & ((1 << per_row_shift) - 1)) * kGroup; }
+  __device__ __forceinline__ int row(int g) const { return row0 + g * row_step; }
 };
 
 // The largest of a job's threads' values (non-negative), of K and of V; every thread of the CTA calls it.  scratch: one per warp.

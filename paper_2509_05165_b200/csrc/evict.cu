@@ -248,7 +248,7 @@ evict_move_kernel(const __grid_constant__ EvictParams P, const int32_t* __restri
     kx[g] = vx[g] = make_uint4(0, 0, 0, 0);
     ks_e[g] = vs_e[g] = kExpMin;
     if (at[g] >= 0) {
-      const long long o = at[g] * P.src.st[2] + j.col(g);
+      const long long o = at[g] * P.src.st[2] + j.col;
       kx[g] = ld16_stream(ks + o);
       vx[g] = ld16_stream(vs + o);
       ks_e[g] = P.src.k_exp[eb + (at[g] >> P.src.block_shift)];
@@ -270,7 +270,7 @@ evict_move_kernel(const __grid_constant__ EvictParams P, const int32_t* __restri
 #pragma unroll
   for (int g = 0; g < 2; ++g) {
     if (at[g] < 0) continue;
-    const long long o = (row0 + j.row(g)) * P.dst.st[2] + j.col(g);
+    const long long o = (row0 + j.row(g)) * P.dst.st[2] + j.col;
     *reinterpret_cast<uint4*>(ko + o) = ks_e[g] == ke ? kx[g] : recode<kFormat>(kx[g], pow2_clamped(ks_e[g] - ke));
     *reinterpret_cast<uint4*>(vo + o) = vs_e[g] == ve ? vx[g] : recode<kFormat>(vx[g], pow2_clamped(vs_e[g] - ve));
   }
