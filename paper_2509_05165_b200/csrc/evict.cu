@@ -2,11 +2,11 @@
 //
 // Two kernels.  evict_select_kernel, a cluster of up to eight CTAs per head: the weights before the protected rows are read
 // once into shared memory, as order-preserving keys, a share per CTA; the key of the last one to keep is found by counting how
-// many lie below seven places of the range that it is in, a third of a digit less each time (eleven steps at most; a
-// histogram of digits is fewer of them, but its atomics crowd into a few bins: 34 us for 64 heads of 32768 rows); the kept
-// positions are written in order.  evict_move_kernel, a job per block of the new cache (see cache8.cuh): kept rows are
+// many lie below seven places of the range that it is in (eleven steps at most; a histogram of digits takes three, but its
+// atomics crowd into a few bins: 34 us for 64 heads of 32768 rows; it is taken for short ones); the kept positions are written in
+// order.  evict_move_kernel, a job per block of the new cache (see cache8.cuh): kept rows are
 // read once, take the exponent of their new block and are written once.
-// B200: 256 heads from 2112 rows to 2048 selection 20 us, moving 48 us (268 MB, 5.6 TB/s); 64 heads of up to 32768 rows to 8192
+// B200: 256 heads from 2112 rows to 2048 selection 12 us, moving 48 us (268 MB, 5.6 TB/s); 64 heads of up to 32768 rows to 8192
 // selection 25 us, moving 18 us.
 #include "cache8.cuh"
 
@@ -16,6 +16,8 @@ namespace {
 constexpr int kSelThreads = 256;        // (1024: a step's barriers wait for 32 warps; 256 heads of 2112 rows 20 -> 53 us with one pivot)
 constexpr int kSelWarps = kSelThreads / 32;
 constexpr int kPivots = 7;
+constexpr int kBins = 8 * kSelThreads;
+constexpr int kSelHistogram = 8192;     // rows of one CTA up to which a histogram of digits is taken (256 heads of 2112 rows 20 -> 12 us)
 constexpr int kSelKeep = 40960;         // keys that a CTA keeps in shared memory (160 KB); what is behind them is read again
 constexpr int kSelCluster = 8;
 
@@ -69,6 +71,8 @@ evict_select_kernel(const __grid_constant__ EvictParams P, int ctas, const float
                     float* __restrict__ weight_out) {
   extern __shared__ __align__(16) uint32_t s_key[];
   __shared__ Exchange x;
+  __shared__ __align__(16) uint32_t hist[kBins];
+  __shared__ int s_bin, s_before;
   grid_dependency_wait();
   const uint32_t rank = ctas == 1 ? 0 : cluster_rank();
   const int unit = blockIdx.x / ctas, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -117,6 +121,54 @@ evict_select_kernel(const __grid_constant__ EvictParams P, int ctas, const float
   int low_count = 0, ties = -1, turn = 0;            // rows below `low`; of the rows with the last key, the first `ties` are kept
   if (ctas > 1)                                      // (a CTA's shared memory is written to by the others once all of them run)
     asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+  if (ctas == 1 && mine <= kSelHistogram) {
+    // digit by digit (11, 11 and 10 bits): the digit that the want-th row has, among the rows with the digits found so far
+    int want_left = want, shift = 32;
+    hi = 0;
+#pragma unroll 1
+    for (int pass = 0; pass < 3; ++pass) {
+      const int bits = pass == 2 ? 10 : 11;
+      const uint32_t fixed = pass == 0 ? 0u : ~0u << shift;
+      shift -= bits;
+      for (int i = tid; i < kBins / 4; i += kSelThreads) reinterpret_cast<uint4*>(hist)[i] = make_uint4(0, 0, 0, 0);
+      __syncthreads();
+      for (int i = tid; i < mine; i += kSelThreads) {
+        const uint32_t key = s_key[i];
+        if (((key ^ hi) & fixed) == 0) atomicAdd(&hist[(key >> shift) & ((1u << bits) - 1)], 1u);
+      }
+      __syncthreads();
+      const uint4 a = reinterpret_cast<const uint4*>(hist)[2 * tid], b = reinterpret_cast<const uint4*>(hist)[2 * tid + 1];
+      const uint32_t bin[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+      uint32_t sum = 0;
+#pragma unroll
+      for (int u = 0; u < 8; ++u) sum += bin[u];
+      uint32_t incl = sum;
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const uint32_t y = __shfl_up_sync(0xffffffffu, incl, o);
+        if (lane >= o) incl += y;
+      }
+      if (lane == 31) x.warp[0][warp][0] = incl;
+      __syncthreads();
+      uint32_t before = incl - sum;
+      for (int w = 0; w < warp; ++w) before += x.warp[0][w][0];
+      if ((int)before < want_left && want_left <= (int)(before + sum)) {
+#pragma unroll
+        for (int u = 0; u < 8; ++u) {
+          if ((int)before < want_left && want_left <= (int)(before + bin[u])) {
+            s_bin = 8 * tid + u;
+            s_before = before;
+          }
+          before += bin[u];
+        }
+      }
+      __syncthreads();
+      hi |= (uint32_t)s_bin << shift;
+      want_left -= s_before;                         // (both written again behind the next barriers)
+    }
+    low = hi;
+    ties = want_left;
+  }
   while (low < hi) {
     const uint32_t range = hi - low, stride = (range >> 3) + 1;
     uint32_t pivot[kPivots], count[kPivots];         // places in (low, hi], keys below them
