@@ -315,6 +315,7 @@ def _attend_plan(cache, q, out, lse, weight, weight_out, row_counts, causal, sca
     _dense(weight, "weight", torch.float32, b, h, cache.capacity)
     _dense(weight_out, "weight_out", torch.float32, b, h, cache.capacity)
     _dense(row_counts, "row_counts", torch.int32, b)
+    _refuse(workspace is not None and not workspace.is_contiguous(), "workspace must be contiguous")
     dev = _one_device(cache.k, q, out, lse, weight, weight_out, row_counts, workspace)
     return C.byref(desc), 0 if workspace is None else workspace.numel() * workspace.element_size(), dev
 
