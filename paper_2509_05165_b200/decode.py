@@ -2,9 +2,9 @@
 
 Same names as the C entry points; tensors are checked for type, shape, layout and device here, values and sizes in the
 library.  A decoding step makes several calls per layer whose kernels take microseconds, so what a combination of types,
-shapes, strides and devices was checked for and turned into is kept (by these, never by a tensor's identity or address) with
-the object that the calls share, and looked up by the next call.  Everything runs on ``stream`` (default: the current one), which has to be a stream of the tensors' device, and
-that device the current one.
+shapes, strides and devices was checked for and turned into is kept (by these and the options' values, never by a tensor's
+identity or address) with the object that the calls share, and looked up by the next call.  Everything runs on ``stream``
+(default: the current one), which has to be a stream of the tensors' device, and that device the current one.
 
     cache = kvc.alloc_cache(batch, n_kv_heads, head_dim, capacity, device=dev)      # one layer
     kvc.kvc_cache_gather(desc, k, v, idx, n_keep, caches)                            # kept rows, all layers
@@ -211,6 +211,7 @@ def kvc_rotary(rope: Rotary, q: Optional[torch.Tensor], k: Optional[torch.Tensor
         q_out = q
     if k_out is None:
         k_out = k
+    inverse = bool(inverse)
     key = (_sig(q), _sig(k), _sig(positions), _sig(q_out), _sig(k_out), inverse)
     plan = rope.plans.get(key) or rope.plans.keep(key, _rotary_plan(q, k, positions, q_out, k_out, inverse))
     _check(_load().kvc_rotary(rope.ref, plan[0], _ptr(q), _ptr(k), positions.data_ptr(), plan[1], _ptr(q_out), _ptr(k_out),
@@ -239,6 +240,7 @@ def kvc_cache_gather(desc, k: Sequence[torch.Tensor], v: Sequence[torch.Tensor],
                      device_status: Optional[torch.Tensor] = None, stream=None) -> None:
     """``kvc_gather`` into 8-bit caches, one per layer.  idx [L, batch, Hkv, N] int32 or None; n_keep [batch, L] (or, with
     ``per_head``, [batch, L, Hkv]) int32 or None.  device_status: int32, becomes KVC_ERR_CAPACITY if rows did not fit."""
+    per_head = bool(per_head)
     key = (bytes(desc), per_head, tuple(map(_sig, k)), tuple(map(_sig, v)), _sig(idx), _sig(n_keep), _sig(device_status),
            tuple([c.device for c in caches]))
     plan = _gather_plans.get(key) or _gather_plans.keep(key, _gather_plan(desc, k, v, idx, n_keep, caches, per_head, device_status))
@@ -328,6 +330,7 @@ def kvc_attend(cache: Cache, q: torch.Tensor, out: torch.Tensor, lse: Optional[t
     weight [batch, Hkv, capacity] fp32: the tokens' running weight, added to in place, or into ``weight_out``."""
     if weight_out is None:
         weight_out = weight
+    causal, scale = bool(causal), float(scale)
     key = ("attend", _sig(q), _sig(out), _sig(lse), _sig(weight), _sig(weight_out), _sig(row_counts), causal, scale, _sig(workspace))
     plan = cache.plans.get(key) or cache.plans.keep(
         key, _attend_plan(cache, q, out, lse, weight, weight_out, row_counts, causal, scale, workspace))
@@ -338,7 +341,7 @@ def kvc_attend(cache: Cache, q: torch.Tensor, out: torch.Tensor, lse: Optional[t
 def _evict_plan(src, dst, weight, budget, idx_out, weight_out):
     b, h = src.batch, src.n_kv_heads
     _dense(weight, "weight", torch.float32, b, h, src.capacity)
-    _dense(idx_out, "idx_out", torch.int32, b, h, int(budget))
+    _dense(idx_out, "idx_out", torch.int32, b, h, budget)
     _dense(weight_out, "weight_out", torch.float32, b, h, dst.capacity)
     return (_one_device(src.k, dst.k, weight, idx_out, weight_out),)
 
@@ -347,7 +350,8 @@ def kvc_evict(src: Cache, dst: Cache, weight: torch.Tensor, budget: int, recent:
               weight_out: Optional[torch.Tensor] = None, stream=None) -> None:
     """The last ``recent`` rows of every head and the heaviest of the others, ``budget`` in all, from src into dst; their
     positions go to idx_out [batch, Hkv, budget] int32, their weights to weight_out [batch, Hkv, dst.capacity]."""
+    budget, recent = int(budget), int(recent)
     key = ("evict", dst.capacity, dst.k.get_device(), _sig(weight), budget, _sig(idx_out), _sig(weight_out))
     plan = src.plans.get(key) or src.plans.keep(key, _evict_plan(src, dst, weight, budget, idx_out, weight_out))
-    _check(_load().kvc_evict(src.ref, dst.ref, weight.data_ptr(), int(budget), int(recent), idx_out.data_ptr(), _ptr(weight_out),
+    _check(_load().kvc_evict(src.ref, dst.ref, weight.data_ptr(), budget, recent, idx_out.data_ptr(), _ptr(weight_out),
                              _launch_stream(plan[0], stream)))

@@ -1,7 +1,6 @@
 """What the decoding calls keep between calls, and what they hand to the library, found on the host (no GPU needed)."""
 import copy
 import math
-import pickle
 
 import pytest
 import torch
@@ -30,3 +29,21 @@ def test_a_workspace_of_repeated_bytes_is_refused():
     assert _status(lambda: kvc.kvc_attend(c, q, q.clone(), workspace=store[at:at + 1].expand(need))) == -1
     wide = torch.zeros((need // 256 + 1, 512), dtype=torch.uint8)
     assert _status(lambda: kvc.kvc_attend(c, q, q.clone(), workspace=wide[:, :256])) == -1
+
+
+def test_options_go_by_their_values():
+    """A number in a tensor that changes between two calls: the second call is checked and made with what it holds then."""
+    c, q = _cache(), torch.zeros((2, 4, 1, 64), dtype=BF)
+    store = torch.zeros(kvc.kvc_attend_workspace_size(c, q, False) + 256, dtype=torch.uint8)
+    ws = store[-store.data_ptr() % 256:]
+    scale = torch.tensor(0.5)
+    gpu = torch.cuda.is_available()
+    first = _status(lambda: kvc.kvc_attend(c, q, q.clone(), scale=scale, workspace=ws))
+    assert first == (-1 if gpu else -4)                     # (host tensors, or no device: past the checks)
+    scale.fill_(math.nan)
+    assert _status(lambda: kvc.kvc_attend(c, q, q.clone(), scale=scale, workspace=ws)) == -1
+    dst, w, idx = _cache(60), torch.zeros((2, 2, 100)), torch.zeros((2, 2, 40), dtype=torch.int32)
+    budget = torch.tensor(40)
+    assert _status(lambda: kvc.kvc_evict(c, dst, w, budget, 4, idx)) == first
+    budget.fill_(50)                                        # idx has no room for as many
+    assert _status(lambda: kvc.kvc_evict(c, dst, w, budget, 4, idx)) == -1
