@@ -178,6 +178,9 @@ class Rotary:
         object.__setattr__(self, "ref", C.byref(rope))
         object.__setattr__(self, "plans", _Plans())
 
+    def __reduce__(self):                # (copies and pickles are made from the fields: the rest holds addresses)
+        return Rotary, tuple(getattr(self, f.name) for f in dataclasses.fields(self))
+
 
 def _rotary_plan(q, k, positions, q_out, k_out, inverse):
     x = q if q is not None else k

@@ -1,6 +1,8 @@
 """What the decoding calls keep between calls, and what they hand to the library, found on the host (no GPU needed)."""
 import copy
+import copy
 import math
+import pickle
 
 import pytest
 import torch
@@ -47,3 +49,14 @@ def test_options_go_by_their_values():
     assert _status(lambda: kvc.kvc_evict(c, dst, w, budget, 4, idx)) == first
     budget.fill_(50)                                        # idx has no room for as many
     assert _status(lambda: kvc.kvc_evict(c, dst, w, budget, 4, idx)) == -1
+
+
+def test_rotary_positions_are_copied_and_pickled():
+    """As part of a model that is copied or sent to another process; the copy turns by the same frequencies, with plans of its own."""
+    rope = kvc.Rotary(64, theta=500000.0, scaling="yarn", factor=16.0, turns_high=32.0, original_ctx=4096.0)
+    q, pos = torch.zeros((1, 2, 3, 64), dtype=BF), torch.arange(3)
+    _status(lambda: kvc.kvc_rotary(rope, q, None, pos))                    # (a plan is kept)
+    for other in (copy.copy(rope), copy.deepcopy({"a": [rope]})["a"][0], pickle.loads(pickle.dumps(rope))):
+        assert other == rope and hash(other) == hash(rope) and other is not rope
+        assert bytes(other.struct) == bytes(rope.struct) and other.plans is not rope.plans and not other.plans
+        assert _status(lambda: kvc.kvc_rotary(other, q, None, pos)) == _status(lambda: kvc.kvc_rotary(rope, q, None, pos))
