@@ -48,7 +48,8 @@ typedef enum {
   KVC_ERR_WORKSPACE = -3,   /* workspace missing, misaligned or smaller than kvc_workspace_size */
   KVC_ERR_CUDA = -4,        /* a CUDA runtime call failed; message in kvc_last_error() */
   KVC_ERR_TIMEOUT = -5,     /* device_status only: a bounded device-side wait gave up */
-  KVC_ERR_CAPACITY = -6     /* device_status only: rows did not fit in a cache (kvc_cache_gather, kvc_cache_append) */
+  KVC_ERR_CAPACITY = -6,    /* device_status only: rows did not fit in a cache (kvc_cache_gather, kvc_cache_append) */
+  KVC_ERR_NOT_FINITE = -7   /* device_status only: rows taken into a cache held infinities or NaN (the same two calls) */
 } kvc_status;
 
 typedef enum { KVC_F32 = 0, KVC_BF16 = 1 } kvc_dtype;
@@ -359,11 +360,14 @@ KVC_API kvc_status kvc_rotary(const kvc_rope* rope, const kvc_rope_desc* desc, c
 
 /*
  * A cache held in 8 bits.  `block` tokens of a head share an exponent, K and V apart: a value is
- * code * 2^exponent.  With amax the largest magnitude in the block, the exponent is the smallest e with
- * amax <= qmax * 2^e (qmax 127 for KVC_INT8, 448 for KVC_E4M3), within [-100, 121]; the code is
- * value * 2^-e rounded to nearest, ties to even.  Powers of two: a value is rounded once, is exact in
- * bf16, and keeps its code's digits when it moves to a block with another exponent, except where that is
- * the larger one.  Rows behind a head's length are never read, and left as they are.
+ * code * 2^exponent.  With amax the largest finite magnitude in the block, the exponent is the smallest e
+ * with amax <= qmax * 2^e (qmax 127 for KVC_INT8, 448 for KVC_E4M3), within [-100, 121]; the code is
+ * value * 2^-e rounded to nearest, ties to even, and held at qmax.  Powers of two: a value is rounded once, is
+ * exact in bf16, and keeps its code's digits when it moves to a block with another exponent, except where
+ * that is the larger one.  Rows behind a head's length are never read, and left as they are.
+ * A cache holds finite numbers: an infinity becomes qmax with its sign, a NaN zero, and the exponent goes by
+ * the values beside them; *device_status of the call that takes them in becomes KVC_ERR_NOT_FINITE unless it
+ * holds an error already.  Codes that a caller writes must not be e4m3's NaN (0x7f, 0xff) or int8's -128.
  */
 typedef enum { KVC_INT8 = 0, KVC_E4M3 = 1 } kvc_cache_format;
 
@@ -385,8 +389,8 @@ typedef struct {
 /* kvc_gather into 8-bit caches, one per layer of desc: row i of head h of layer l becomes
  * K[l][b, h, idx[l, b, h, i]] for i < n_keep, V alike, and lengths is set.  idx [L, batch, Hkv, N] may be NULL
  * (row i is token i).  n_keep: [batch, L], or with per_head [batch, L, Hkv]; NULL keeps all N.  A layer that keeps
- * more rows than its cache's capacity keeps the first ones, and *device_status (may be NULL; written only then)
- * becomes KVC_ERR_CAPACITY.  An idx entry outside [0, N) gives a row of zeros.  caches: HOST array of L. */
+ * more rows than its cache's capacity keeps the first ones, and *device_status (may be NULL; written only then, and for
+ * rows that are not finite, see above) becomes KVC_ERR_CAPACITY.  An idx entry outside [0, N) gives a row of zeros.  caches: HOST array of L. */
 KVC_API kvc_status kvc_cache_gather(const kvc_desc* desc, const void* const* k, const void* const* v, const int32_t* idx,
                                     const int32_t* n_keep, int32_t per_head, const kvc_cache* caches,
                                     int32_t* device_status, void* stream);
@@ -396,7 +400,8 @@ KVC_API kvc_status kvc_cache_gather(const kvc_desc* desc, const void* const* k, 
  * a padded batch).  The open block's exponent grows if the new rows need it (its codes are then rounded again), a
  * block that starts takes the exponent of its rows.  lengths_out: the lengths afterwards, [batch, Hkv]; NULL writes
  * them to cache->lengths.  weight (may be NULL): fp32 [batch, Hkv, capacity], set to 0 for the new rows.  Rows
- * that do not fit are dropped, and *device_status (may be NULL; written only then) becomes KVC_ERR_CAPACITY. */
+ * that do not fit are dropped, and *device_status (may be NULL; written only then, and for rows that are not finite, see
+ * above) becomes KVC_ERR_CAPACITY. */
 KVC_API kvc_status kvc_cache_append(const kvc_cache* cache, const void* k_new, const void* v_new, int32_t dtype,
                                     int32_t rows, const int64_t* stride, const int32_t* n_new, int32_t* lengths_out,
                                     float* weight, int32_t* device_status, void* stream);

@@ -16,7 +16,8 @@ AGG_MAX, AGG_MEAN = 0, 1
 KVC_MAX_LAYERS = 128
 
 _STATUS = {0: "KVC_OK", -1: "KVC_ERR_INVALID_ARG", -2: "KVC_ERR_UNSUPPORTED", -3: "KVC_ERR_WORKSPACE",
-           -4: "KVC_ERR_CUDA", -5: "KVC_ERR_TIMEOUT", -6: "KVC_ERR_CAPACITY"}
+           -4: "KVC_ERR_CUDA", -5: "KVC_ERR_TIMEOUT", -6: "KVC_ERR_CAPACITY",
+           -7: "KVC_ERR_NOT_FINITE"}
 
 
 class KvcError(RuntimeError):

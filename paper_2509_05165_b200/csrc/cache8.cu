@@ -44,7 +44,7 @@ cache_gather_kernel(const __grid_constant__ CacheGatherParams P, const int32_t* 
   const int n = (int)min(kept, y.cap);                 // (capacities are below 2^31 - 1024)
   if (blockIdx.x == 0 && threadIdx.x == 0) {
     y.lengths[unit] = n;
-    if (kept > n && device_status != nullptr) *device_status = KVC_ERR_CAPACITY;
+    if (kept > n && device_status != nullptr) atomicExch(device_status, KVC_ERR_CAPACITY);
   }
 
   const JobLane<8> j(P.block_shift, P.d);
@@ -82,17 +82,34 @@ cache_gather_kernel(const __grid_constant__ CacheGatherParams P, const int32_t* 
     km = kx[g].max_bits(km);
     vm = vx[g].max_bits(vm);
   }
-  const float2 top = job_max(make_float2(Raw8<T>::top(km), Raw8<T>::top(vm)), j, scratch);
+  float2 top = job_max(make_float2(Raw8<T>::top(km), Raw8<T>::top(vm)), j, scratch);
   if (row0 >= n) return;
+  // the thread's row g: its token's place among the values (as above), -1 if there is none
+  const auto row = [&](int g) -> long long {
+    if (g * j.row_step >= left) return -1;
+    const int t = map == nullptr ? row0 + j.row(g) : map[g * j.row_step];
+    return t < 0 || t >= P.N ? -1 : t * P.kvs[2];
+  };
+  const bool finite = all_finite(top);
+  if (!finite) top = finite_max(ks, vs, row, j, scratch, device_status);
   const int ke = exponent_of<kFormat>(top.x), ve = exponent_of<kFormat>(top.y);
   const float kf = pow2(-ke), vf = pow2(-ve);
   long long to = b * y.st[0] + h * y.st[1] + (row0 + j.row0) * y.st[2] + j.col;
   const long long step = j.row_step * y.st[2];
+  if (finite) {
 #pragma unroll
-  for (int g = 0; g < 4; ++g, to += step) {
-    if (g * j.row_step < left) {
-      *reinterpret_cast<uint2*>(y.ko + to) = kx[g].template encode<kFormat>(kf);
-      *reinterpret_cast<uint2*>(y.vo + to) = vx[g].template encode<kFormat>(vf);
+    for (int g = 0; g < 4; ++g, to += step) {
+      if (g * j.row_step < left) {
+        *reinterpret_cast<uint2*>(y.ko + to) = kx[g].template encode<kFormat>(kf);
+        *reinterpret_cast<uint2*>(y.vo + to) = vx[g].template encode<kFormat>(vf);
+      }
+    }
+  } else {
+#pragma unroll 1
+    for (int g = 0; g * j.row_step < left && g < 4; ++g, to += step) {
+      const long long o = row(g);
+      *reinterpret_cast<uint2*>(y.ko + to) = o < 0 ? make_uint2(0, 0) : encode_any<kFormat>(ks + o, kf);
+      *reinterpret_cast<uint2*>(y.vo + to) = o < 0 ? make_uint2(0, 0) : encode_any<kFormat>(vs + o, vf);
     }
   }
   if (j.t == 0) {
@@ -141,7 +158,7 @@ cache_append_kernel(const __grid_constant__ AppendParams P, const T* __restrict_
   __syncthreads();                       // every thread has the length before it may change
   if (blockIdx.x == 0 && threadIdx.x == 0) {
     if (P.write_lengths) lengths_out[unit] = len + n;
-    if (n < want && device_status != nullptr) *device_status = KVC_ERR_CAPACITY;
+    if (n < want && device_status != nullptr) atomicExch(device_status, KVC_ERR_CAPACITY);
   }
   if (n == 0) return;
   const JobLane<8> j(c.block_shift, c.d);
@@ -172,8 +189,16 @@ cache_append_kernel(const __grid_constant__ AppendParams P, const T* __restrict_
       km = kx[g].max_bits(km);
       vm = vx[g].max_bits(vm);
     }
-    const float2 top = job_max(make_float2(Raw8<T>::top(km), Raw8<T>::top(vm)), j, scratch);
+    float2 top = job_max(make_float2(Raw8<T>::top(km), Raw8<T>::top(vm)), j, scratch);
     if (!live) continue;
+    const bool finite = all_finite(top);
+    if (!finite) {
+      const auto row = [&](int g) -> long long {
+        const int r = row0 + j.row(g) - len;
+        return r >= 0 && r < n ? from + r * P.ns[2] + j.col : -1;
+      };
+      top = finite_max(k_new, v_new, row, j, scratch, device_status);
+    }
     const long long eat = (long long)unit * c.blocks + blk;
     int ke = exponent_of<kFormat>(top.x), ve = exponent_of<kFormat>(top.y);
     const bool open = row0 < len;                         // the block has rows already
@@ -190,6 +215,12 @@ cache_append_kernel(const __grid_constant__ AppendParams P, const T* __restrict_
       const int r = row0 + j.row(g);
       const long long o = to + r * c.st[2] + j.col;
       if (r >= len && r < len + n) {
+        if (!finite) {                                      // (some of the job's values: read again)
+          const long long at = from + (r - len) * P.ns[2] + j.col;
+          *reinterpret_cast<uint2*>(c.k + o) = encode_any<kFormat>(k_new + at, pow2(-ke));
+          *reinterpret_cast<uint2*>(c.v + o) = encode_any<kFormat>(v_new + at, pow2(-ve));
+          continue;
+        }
         *reinterpret_cast<uint2*>(c.k + o) = kx[g].template encode<kFormat>(pow2(-ke));
         *reinterpret_cast<uint2*>(c.v + o) = vx[g].template encode<kFormat>(pow2(-ve));
       } else if (open && r < len && (ke > kwas || ve > vwas)) {      // a code under a larger exponent: rounded again
@@ -198,7 +229,7 @@ cache_append_kernel(const __grid_constant__ AppendParams P, const T* __restrict_
       }
     }
     // every thread of the job has read the old exponents before they change
-    if (j.threads == 32) __syncwarp(); else asm volatile("bar.sync %0, %1;" :: "r"(1 + j.slot), "r"(j.threads) : "memory");
+    job_barrier(j);
     if (j.t == 0) {
       c.k_exp[eat] = (int8_t)ke;
       c.v_exp[eat] = (int8_t)ve;

@@ -138,23 +138,33 @@ struct JobLane {
   __device__ __forceinline__ int row(int g) const { return row0 + g * row_step; }
 };
 
-// The largest of a job's threads' values (non-negative), of K and of V; every thread of the CTA calls it.  scratch: one per warp.
+// A job's threads meet (a warp, or whole warps: barrier 1 + slot).
 template <typename Job>
-__device__ __forceinline__ float2 job_max(float2 x, const Job& j, float2* scratch) {
-  x.x = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(x.x)));
-  x.y = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(x.y)));
-  if (j.threads == 32) return x;
-  __syncthreads();                        // (the scratch of the call before has been read)
-  if ((threadIdx.x & 31) == 0) scratch[threadIdx.x >> 5] = x;
-  __syncthreads();
-  const int w0 = j.slot * (j.threads >> 5);
-  x = scratch[w0];
-  for (int i = 1; i < (j.threads >> 5); ++i) {
-    x.x = fmaxf(x.x, scratch[w0 + i].x);
-    x.y = fmaxf(x.y, scratch[w0 + i].y);
-  }
-  return x;
+__device__ __forceinline__ void job_barrier(const Job& j) {
+  if (j.threads == 32) __syncwarp();
+  else asm volatile("bar.sync %0, %1;" :: "r"(1 + j.slot), "r"(j.threads) : "memory");
 }
+
+// The largest of a job's threads' values, of K and of V: non-negative, and compared by their bits, in which NaN is above infinity.
+// kTogether: every thread of the CTA calls it; else whole jobs do.  scratch: one per warp.
+template <bool kTogether = true, typename Job>
+__device__ __forceinline__ float2 job_max(float2 x, const Job& j, float2* scratch) {
+  uint32_t k = __reduce_max_sync(0xffffffffu, __float_as_uint(x.x)), v = __reduce_max_sync(0xffffffffu, __float_as_uint(x.y));
+  if (j.threads > 32) {
+    const auto meet = [&] { if (kTogether) __syncthreads(); else job_barrier(j); };
+    meet();                               // (the scratch of the call before has been read)
+    if ((threadIdx.x & 31) == 0) scratch[threadIdx.x >> 5] = make_float2(__uint_as_float(k), __uint_as_float(v));
+    meet();
+    const int w0 = j.slot * (j.threads >> 5);
+    for (int i = 0; i < (j.threads >> 5); ++i) {
+      k = max(k, __float_as_uint(scratch[w0 + i].x));
+      v = max(v, __float_as_uint(scratch[w0 + i].y));
+    }
+  }
+  return make_float2(__uint_as_float(k), __uint_as_float(v));
+}
+
+__device__ __forceinline__ bool all_finite(float2 top) { return max(__float_as_uint(top.x), __float_as_uint(top.y)) < 0x7f800000u; }
 
 // Eight values as they lie in memory.
 template <typename T>
@@ -195,6 +205,24 @@ struct Raw8 {
     for (int i = 0; i < (int)sizeof(T) * 2; ++i) m = sizeof(T) == 2 ? __vmaxu2(m, u[i] & 0x7fff7fffu) : max(m, u[i] & 0x7fffffffu);
     return m;
   }
+  // max_bits of the finite values; NaN become zero.
+  __device__ __forceinline__ uint32_t max_finite_bits(uint32_t m) {
+    uint32_t* u = &w[0].x;
+#pragma unroll
+    for (int i = 0; i < (int)sizeof(T) * 2; ++i) {
+      if (sizeof(T) == 2) {
+        const uint32_t lo = u[i] & 0x7fffu, hi = (u[i] >> 16) & 0x7fffu;
+        if (lo > 0x7f80u) u[i] &= 0xffff0000u;
+        if (hi > 0x7f80u) u[i] &= 0x0000ffffu;
+        m = __vmaxu2(m, (lo < 0x7f80u ? lo : 0u) | (hi < 0x7f80u ? hi << 16 : 0u));
+      } else {
+        const uint32_t mag = u[i] & 0x7fffffffu;
+        if (mag > 0x7f800000u) u[i] = 0;
+        if (mag < 0x7f800000u) m = max(m, mag);
+      }
+    }
+    return m;
+  }
   static __device__ __forceinline__ float top(uint32_t m) {
     return __uint_as_float(sizeof(T) == 2 ? max(m << 16, m & 0xffff0000u) : m);
   }
@@ -205,6 +233,34 @@ struct Raw8 {
     return make_uint2(encode4<kFormat>(x[0], x[1], x[2], x[3], f), encode4<kFormat>(x[4], x[5], x[6], x[7], f));
   }
 };
+
+// A job's largest values where some are not finite: of the finite ones.  The rows are read again, one at a time, so that the
+// way without such rows keeps its registers (64; with the rows kept for both, 97).  row(g): where row g of the thread lies, -1 if
+// there is none.  The status word, if it holds no error yet, says so.  Whole jobs call it.
+template <typename T, typename Job, typename Row>
+__device__ __forceinline__ float2 finite_max(const T* k, const T* v, const Row& row, const Job& j, float2* scratch, int32_t* device_status) {
+  if (j.t == 0 && device_status != nullptr) atomicCAS(device_status, KVC_OK, KVC_ERR_NOT_FINITE);
+  uint32_t km = 0, vm = 0;
+#pragma unroll 1
+  for (int g = 0; g < 4; ++g) {
+    const long long at = row(g);
+    if (at < 0) continue;
+    Raw8<T> x;
+    x.load(k + at);
+    km = x.max_finite_bits(km);
+    x.load(v + at);
+    vm = x.max_finite_bits(vm);
+  }
+  return job_max<false>(make_float2(Raw8<T>::top(km), Raw8<T>::top(vm)), j, scratch);
+}
+// Codes of eight such values: a NaN is taken as zero, an infinity is held at the largest code.
+template <int kFormat, typename T>
+__device__ __forceinline__ uint2 encode_any(const T* p, float f) {
+  Raw8<T> x;
+  x.load(p);
+  x.max_finite_bits(0);
+  return x.template encode<kFormat>(f);
+}
 
 // Sixteen codes rounded again after a change of exponent.
 template <int kFormat>

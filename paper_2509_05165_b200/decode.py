@@ -242,7 +242,8 @@ def kvc_cache_gather(desc, k: Sequence[torch.Tensor], v: Sequence[torch.Tensor],
                      n_keep: Optional[torch.Tensor], caches: Sequence[Cache], per_head: bool = False,
                      device_status: Optional[torch.Tensor] = None, stream=None) -> None:
     """``kvc_gather`` into 8-bit caches, one per layer.  idx [L, batch, Hkv, N] int32 or None; n_keep [batch, L] (or, with
-    ``per_head``, [batch, L, Hkv]) int32 or None.  device_status: int32, becomes KVC_ERR_CAPACITY if rows did not fit."""
+    ``per_head``, [batch, L, Hkv]) int32 or None.  device_status: int32, becomes KVC_ERR_CAPACITY if rows did not fit, KVC_ERR_NOT_FINITE (over 0 only)
+    if kept rows held infinities or NaN."""
     per_head = bool(per_head)
     key = (bytes(desc), per_head, tuple(map(_sig, k)), tuple(map(_sig, v)), _sig(idx), _sig(n_keep), _sig(device_status),
            tuple([c.device for c in caches]))
@@ -269,7 +270,8 @@ def _append_plan(cache, k_new, v_new, n_new, lengths_out, weight, device_status)
 def kvc_cache_append(cache: Cache, k_new: torch.Tensor, v_new: torch.Tensor, n_new: Optional[torch.Tensor] = None,
                      lengths_out: Optional[torch.Tensor] = None, weight: Optional[torch.Tensor] = None,
                      device_status: Optional[torch.Tensor] = None, stream=None) -> None:
-    """Rows of new tokens [batch, Hkv, rows, head_dim] behind the ones in use; ``n_new`` [batch] int32 of them per sequence."""
+    """Rows of new tokens [batch, Hkv, rows, head_dim] behind the ones in use; ``n_new`` [batch] int32 of them per sequence.
+    device_status as in ``kvc_cache_gather``."""
     key = ("append", _sig(k_new), _sig(v_new), _sig(n_new), _sig(lengths_out), _sig(weight), _sig(device_status))
     plan = cache.plans.get(key) or cache.plans.keep(key, _append_plan(cache, k_new, v_new, n_new, lengths_out, weight, device_status))
     _check(_load().kvc_cache_append(cache.ref, k_new.data_ptr(), v_new.data_ptr(), plan[0], plan[1], plan[2], _ptr(n_new), _ptr(lengths_out),

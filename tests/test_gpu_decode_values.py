@@ -1,10 +1,12 @@
-"""Values at the ends of their types' range in the 8-bit cache and its attention."""
+"""Values at the ends of their types' range, and rows that are not finite, in the 8-bit cache."""
+import math
 
 import pytest
 import torch
 
+import decode_ref as R
 import paper_2509_05165_b200 as kvc
-from test_gpu_decode import E4, I8, _bits, _gen, dev  # noqa: F401
+from test_gpu_decode import BF, E4, F32, I8, _bits, _check_attend, _gen, dev  # noqa: F401
 
 pytestmark = pytest.mark.gpu
 
@@ -29,3 +31,118 @@ def test_evict_blocks_of_the_largest_exponent(dev, fmt):
         for a, b in ((c.k, dst.k), (c.v, dst.v)):
             assert torch.equal(_bits(b)[0, j], _bits(a)[0, j][kept])
     assert (dst.k_exp[..., :3] == 121).all() and (dst.v_exp[..., :3] == 121).all()
+
+
+# ---- rows that are not finite ------------------------------------------------------------------------------------------
+
+def _held(x, fmt):
+    """Codes and exponent of a block's rows: the exponent by the finite values; infinities take the largest code, NaN zero."""
+    x = x.double()
+    fin = torch.where(torch.isfinite(x), x, torch.zeros_like(x))
+    e = R.exponent(float(fin.abs().max()) if x.numel() else 0.0, fmt)
+    return R.round_code(torch.nan_to_num(x, nan=0.0, posinf=math.inf, neginf=-math.inf) * 2.0 ** -e, fmt), e
+
+
+def _spoil(x, dtype):
+    """Infinities of both signs and NaN in some rows; blocks with nothing else; the type's largest value beside others."""
+    x = x.clone()
+    x[..., 3, 5], x[..., 4, 0], x[..., 5, -1] = math.inf, -math.inf, math.nan
+    x[..., 40, 7] = math.nan
+    x[..., 128:160, :] = math.nan
+    x[..., 130, :], x[..., 131, :] = math.inf, -math.inf
+    x[..., 190, 1] = torch.finfo(dtype).max / 4
+    x[..., 191, 2] = -math.inf
+    return x
+
+
+@pytest.mark.parametrize("fmt", [I8, E4])
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("d,block", [(64, 16), (128, 32), (64, 64), (128, 128)])
+def test_gather_of_rows_that_are_not_finite(dev, fmt, dtype, d, block):
+    """Every value beside them keeps its place and size, and the call says so in its status; rows that are not kept do not matter."""
+    h, n = 2, 300
+    g = _gen(block)
+    k, v = [_spoil(R.spread_rows(g, 1, h, n, d), dtype).to(dtype) for _ in range(2)]
+    desc = kvc.kvc_desc_init(1, 1, h, h, d, n, 1, kvc.F32 if dtype == F32 else kvc.BF16)
+    c = kvc.alloc_cache(1, h, d, n, block, fmt, dev)
+    status = torch.zeros(1, dtype=torch.int32, device=dev)
+    kvc.kvc_cache_gather(desc, [k.to(dev)], [v.to(dev)], None, None, [c], device_status=status)
+    for j in range(h):
+        for codes, exps, x in ((c.k, c.k_exp, k), (c.v, c.v_exp, v)):
+            for r in range(-(-n // block)):
+                want, e = _held(x[0, j, r * block:(r + 1) * block], fmt)
+                assert int(exps[0, j, r]) == e, (j, r)
+                assert torch.equal(codes[0, j, r * block:(r + 1) * block].cpu().double(), want), (j, r)
+    assert int(status) == -7
+    # what was there before stays but for "no error", and rows that did not fit say more
+    status.fill_(-6)
+    kvc.kvc_cache_gather(desc, [k.to(dev)], [v.to(dev)], None, None, [c], device_status=status)
+    assert int(status) == -6
+    status.zero_()
+    small = kvc.alloc_cache(1, h, d, 200, block, fmt, dev)
+    kvc.kvc_cache_gather(desc, [k.to(dev)], [v.to(dev)], None, None, [small], device_status=status)
+    assert int(status) == -6
+    status.zero_()
+    idx = torch.cat([torch.arange(6, 40), torch.arange(41, 128), torch.arange(192, n), torch.arange(6), torch.tensor([40]), torch.arange(128, 192)])
+    idx = idx.to(torch.int32).expand(1, 1, h, n).contiguous().to(dev)
+    kvc.kvc_cache_gather(desc, [k.to(dev)], [v.to(dev)], idx, torch.full((1, 1), 229, dtype=torch.int32, device=dev), [c], device_status=status)
+    assert int(status) == 0
+
+
+@pytest.mark.parametrize("fmt", [I8, E4])
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("d,block,rows", [(64, 16, 1), (128, 32, 7), (64, 128, 1), (128, 128, 130), (128, 64, 400), (64, 16, 400)])
+def test_append_of_rows_that_are_not_finite(dev, fmt, dtype, d, block, rows):
+    """The rows that an open block holds already are left alone, the ordinary new values beside theirs are kept."""
+    b, h, have = 2, 2, block // 2 + 1
+    g = _gen(rows)
+    c = kvc.alloc_cache(b, h, d, have + rows + 3, block, fmt, dev)
+    old = [R.spread_rows(g, b, h, have, d).to(dtype) for _ in range(2)]
+    status = torch.zeros(1, dtype=torch.int32, device=dev)
+    kvc.kvc_cache_append(c, old[0].to(dev), old[1].to(dev), device_status=status)
+    assert int(status) == 0
+    new = [0.25 * torch.randn((b, h, rows, d), generator=g).to(dtype) for _ in range(2)]
+    new[0][0, 0, 0, 3], new[0][0, 1, rows - 1, d - 1], new[1][0, 0, rows // 2, 0], new[1][0, 1, 0, 8] = math.inf, math.nan, -math.inf, math.nan
+    kvc.kvc_cache_append(c, new[0].to(dev), new[1].to(dev), device_status=status, n_new=torch.tensor([rows, 0], dtype=torch.int32, device=dev))
+    assert int(status) == -7
+    for j in range(h):
+        for codes, exps, was, x in ((c.k, c.k_exp, old[0], new[0]), (c.v, c.v_exp, old[1], new[1])):
+            first, e0 = _held(was[0, j, :block], fmt)
+            assert have < block
+            room = min(block - have, rows)
+            _, e1 = _held(x[0, j, :room], fmt)
+            e = max(e0, e1)
+            if e > e0:
+                first = R.round_code(first * 2.0 ** max(e0 - e, -126), fmt)
+            ordinary = torch.nan_to_num(x[0, j].double(), nan=0.0, posinf=math.inf, neginf=-math.inf)
+            want = [torch.cat([first, R.round_code(ordinary[:room] * 2.0 ** -e, fmt)])]
+            assert int(exps[0, j, 0]) == e
+            for r in range(room, rows, block):
+                w, e = _held(x[0, j, r:r + block], fmt)
+                want.append(w)
+                assert int(exps[0, j, (have + r) // block]) == e
+            assert torch.equal(codes[0, j, :have + rows].cpu().double(), torch.cat(want)), j
+    assert (c.lengths.cpu() == torch.tensor([[have + rows] * h, [have] * h])).all()
+    # the second sequence's rows of this call are padding: NaN there is not looked at
+    status.zero_()
+    for x in new:
+        x[0], x[1] = 0.5, math.nan
+    c.lengths.fill_(1)
+    kvc.kvc_cache_append(c, new[0].to(dev), new[1].to(dev), device_status=status, n_new=torch.tensor([rows, 0], dtype=torch.int32, device=dev))
+    assert int(status) == 0
+
+
+@pytest.mark.parametrize("fmt", [I8, E4])
+def test_attention_over_rows_that_were_not_finite(dev, fmt):
+    """A NaN in the last token leaves rows that do not see that token as they are, and no output is NaN: it is held as zero."""
+    g = _gen(9)
+    k, v = [torch.randn((1, 2, 50, 64), generator=g).to(BF) for _ in range(2)]
+    k[..., 49, 3], v[..., 49, 5], k[..., 48, 0] = math.nan, math.nan, math.inf
+    c = kvc.alloc_cache(1, 2, 64, 60, 16, fmt, dev)
+    kvc.kvc_cache_append(c, k.to(dev), v.to(dev))
+    q = torch.randn((1, 4, 3, 64), generator=g).to(BF).to(dev)
+    out, lse = torch.empty_like(q), torch.empty((1, 4, 3), device=dev)
+    w = torch.full((1, 2, 60), -9.0, device=dev)
+    ws = torch.empty(kvc.kvc_attend_workspace_size(c, q, True), dtype=torch.uint8, device=dev)
+    kvc.kvc_attend(c, q, out, lse, weight_out=w, workspace=ws)
+    _check_attend(c, q, out, lse, w, torch.zeros_like(w), True, 1 / 8.0)
