@@ -434,8 +434,9 @@ KVC_API kvc_status kvc_attend_workspace_size(const kvc_cache* cache, const kvc_a
  * batch); the others' outputs are left as they were, and they weigh nothing.  weight_out (may be NULL): fp32 [batch,
  * Hkv, capacity]; weight_out[b, h, c] = weight_in[b, h, c] + sum of p[c] over the rows and the query heads of KV
  * head h, for every c in use; weight_in may be weight_out, or NULL for zeros.  Sums are taken in a fixed order.
- * batch * n_kv_heads * capacity must be below 2^34.  Query rows are taken 64 per KV head and launch: the call is meant
- * for decoded, drafted or a turn's tokens. */
+ * A query row that holds an infinity or NaN gives NaN: its outputs, its lse and, with weight_out, the weights of its KV
+ * head's tokens; unless it sees no token.  batch * n_kv_heads * capacity must be below 2^34.  Query rows are taken 64 per
+ * KV head and launch: the call is meant for decoded, drafted or a turn's tokens. */
 KVC_API kvc_status kvc_attend(const kvc_cache* cache, const kvc_attend_desc* desc, const void* q, const int32_t* row_counts,
                               void* out, float* lse, const float* weight_in, float* weight_out, void* workspace,
                               size_t workspace_bytes, void* stream);

@@ -355,7 +355,8 @@ attend_split_kernel(const __grid_constant__ AttendParams P, const T* __restrict_
       top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
       top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
       const int e = min(max((int)(__float_as_uint(top) >> 23) - 127, -120), 126);
-      const float down = pow2(-e), up = pow2(e) * P.scale * 1.44269504088896341f;
+      // (an infinity makes the whole row NaN, as one does by itself; fmaxf passes NaN over)
+      const float down = __float_as_uint(top) < 0x7f800000u ? pow2(-e) : __int_as_float(0x7fffffff), up = pow2(e) * P.scale * 1.44269504088896341f;
 #pragma unroll
       for (int s = 0; s < kSteps; ++s) {
         uint32_t w[2];
@@ -784,7 +785,8 @@ attend_join_kernel(const __grid_constant__ AttendParams P, const int32_t* __rest
     l += ml.y * f;
     a.x += y.x * f; a.y += y.y * f; a.z += y.z * f; a.w += y.w * f;
   }
-  const float inv = l > 0.f ? 1.f / l : 0.f;
+  const bool none = l == 0.f;                          // (the row sees no token; a sum of NaN stays one)
+  const float inv = none ? 0.f : 1.f / l;
   // place 8 k + g holds entries (kD / 8) g + 4 k ..
   T* dst = out + b * P.os[0] + j * P.os[1] + mm * P.os[2] + (kD / 8) * (at & 7) + 4 * (at >> 3);
   a.x *= inv; a.y *= inv; a.z *= inv; a.w *= inv;
@@ -794,9 +796,9 @@ attend_join_kernel(const __grid_constant__ AttendParams P, const int32_t* __rest
   } else {
     *reinterpret_cast<float4*>(dst) = a;
   }
-  if (at == 0) P.lse2[(long long)unit * P.live + r1] = l > 0.f ? top + log2f(l) : INFINITY;
+  if (at == 0) P.lse2[(long long)unit * P.live + r1] = none ? INFINITY : top + log2f(l);
   if (at == 0 && lse != nullptr)
-    lse[((long long)b * P.Hq + j) * P.rows + mm] = l > 0.f ? (top + log2f(l)) * 0.693147180559945309f : -INFINITY;
+    lse[((long long)b * P.Hq + j) * P.rows + mm] = none ? -INFINITY : (top + log2f(l)) * 0.693147180559945309f;
 }
 
 // weight_out = weight_in + the sum of 2^(logit - log-sum-exp) over the rows: four tokens of a head per thread.

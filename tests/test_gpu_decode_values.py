@@ -1,4 +1,4 @@
-"""Values at the ends of their types' range, and rows that are not finite, in the 8-bit cache."""
+"""Values at the ends of their types' range, and rows that are not finite, in the 8-bit cache and its attention."""
 import math
 
 import pytest
@@ -6,7 +6,7 @@ import torch
 
 import decode_ref as R
 import paper_2509_05165_b200 as kvc
-from test_gpu_decode import BF, E4, F32, I8, _bits, _check_attend, _gen, dev  # noqa: F401
+from test_gpu_decode import BF, E4, F32, I8, _bits, _check_attend, _filled_cache, _gen, dev  # noqa: F401
 
 pytestmark = pytest.mark.gpu
 
@@ -145,4 +145,30 @@ def test_attention_over_rows_that_were_not_finite(dev, fmt):
     w = torch.full((1, 2, 60), -9.0, device=dev)
     ws = torch.empty(kvc.kvc_attend_workspace_size(c, q, True), dtype=torch.uint8, device=dev)
     kvc.kvc_attend(c, q, out, lse, weight_out=w, workspace=ws)
+    _check_attend(c, q, out, lse, w, torch.zeros_like(w), True, 1 / 8.0)
+
+
+# ---- attention ---------------------------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("rows", [1, 3, 9])
+@pytest.mark.parametrize("bad", [math.nan, math.inf, -math.inf])
+def test_a_query_row_that_is_not_finite_gives_nan_and_no_other_row_does(dev, dtype, rows, bad):
+    """Its outputs, its log-sum-exp (-inf would say that it sees no token) and the weights of its KV head; the rest is untouched."""
+    g = _gen(rows)
+    c = _filled_cache(dev, g, 2, 2, 64, 300, 32, I8, torch.tensor([[300, 200], [130, 0]]))
+    q = torch.randn((2, 6, rows, 64), generator=g).to(dtype).to(dev)
+    spoilt = q.clone()
+    spoilt[0, 1, rows - 1, 7] = bad
+    spoilt[1, 5, rows - 1] = bad                             # sees no token: zeros and -inf, whatever it holds
+    ws = torch.empty(kvc.kvc_attend_workspace_size(c, q, True), dtype=torch.uint8, device=dev)
+    got = []
+    for x in (q, spoilt):
+        out, lse, w = torch.empty_like(q), torch.empty((2, 6, rows), device=dev), torch.full((2, 2, 300), -9.0, device=dev)
+        kvc.kvc_attend(c, x, out, lse, weight_out=w, workspace=ws)
+        got.append((out, lse, w))
+    (o0, l0, w0), (out, lse, w) = got
+    assert torch.isnan(out[0, 1, rows - 1]).all() and torch.isnan(lse[0, 1, rows - 1]) and torch.isnan(w[0, 0]).all()
+    assert (out[1, 3:] == 0).all() and torch.isneginf(lse[1, 3:]).all()
+    out[0, 1, rows - 1], lse[0, 1, rows - 1], w[0, 0] = o0[0, 1, rows - 1], l0[0, 1, rows - 1], w0[0, 0]
     _check_attend(c, q, out, lse, w, torch.zeros_like(w), True, 1 / 8.0)
