@@ -435,8 +435,13 @@ KVC_API kvc_status kvc_attend_workspace_size(const kvc_cache* cache, const kvc_a
  * Hkv, capacity]; weight_out[b, h, c] = weight_in[b, h, c] + sum of p[c] over the rows and the query heads of KV
  * head h, for every c in use; weight_in may be weight_out, or NULL for zeros.  Sums are taken in a fixed order.
  * A query row that holds an infinity or NaN gives NaN: its outputs, its lse and, with weight_out, the weights of its KV
- * head's tokens; unless it sees no token.  batch * n_kv_heads * capacity must be below 2^34.  Query rows are taken 64 per
- * KV head and launch: the call is meant for decoded, drafted or a turn's tokens. */
+ * head's tokens; unless it sees no token.
+ * Precision: sums are fp32 (logits and V's values should stay below 2^90).  Products take fp16 operands, in which codes
+ * are exact.  A row of q in bf16 is exact but for entries 2^17 times below its largest; in fp32 it is within 2^-23 of its
+ * largest.  In front of v, p is rounded to 11 bits where dtype is bf16 (off by at most 2^-11 of sum p |v|, where the
+ * output's rounding is 2^-8 of its value) and to 22 where it is fp32; lse and weight_out take it unrounded.
+ * batch * n_kv_heads * capacity must be below 2^34.  Query rows are taken 64 per KV head and launch, each of which reads
+ * the cache: the call is meant for decoded, drafted or a turn's tokens. */
 KVC_API kvc_status kvc_attend(const kvc_cache* cache, const kvc_attend_desc* desc, const void* q, const int32_t* row_counts,
                               void* out, float* lse, const float* weight_in, float* weight_out, void* workspace,
                               size_t workspace_bytes, void* stream);
@@ -445,7 +450,7 @@ KVC_API kvc_status kvc_attend(const kvc_cache* cache, const kvc_attend_desc* des
  * among the others are kept, `budget` in all (all of them where no more are in use), in their order.  Equal weights
  * keep the smaller position first.  The kept rows become dst's rows, weights go to weight_out [batch, Hkv,
  * dst->capacity] (may be NULL), dst->lengths is set, and idx_out [batch, Hkv, budget] int32 holds the kept
- * positions, then -1.  src and dst (same batch, heads, head_dim and format; not the same memory) may differ in block
+ * positions, then -1.  src and dst (same batch, heads, head_dim and format; the spans of their arrays do not overlap) may differ in block
  * and capacity; 1 <= budget <= dst->capacity, 0 <= recent <= budget.  weight: fp32 [batch, Hkv, src->capacity],
  * not NaN. */
 KVC_API kvc_status kvc_evict(const kvc_cache* src, const kvc_cache* dst, const float* weight, int64_t budget, int64_t recent,

@@ -20,8 +20,10 @@
 //   softmax's denominator is known only after the last token).
 //
 // Numbers: codes are exact in fp16.  A query row is scaled by a power of two to below 2 and rounded to fp16, which is exact
-// for bf16 but for entries 2^14 times smaller than the row's largest; fp32 rows go as two fp16 (22 bits), and so does P in
-// front of V then (one fp16, 11 bits, for bf16 outputs).  Products, softmax and sums are fp32.  V's exponents differ from block
+// for bf16 but for entries 2^17 times smaller than the row's largest (fp16's smallest step is 2^-24, a bf16 has 8 bits); fp32
+// rows go as two fp16 (within 2^-23 of the row's largest entry), and so does P in front of V then (22 bits).  For bf16 outputs P is
+// one fp16: 11 bits, off by at most 2^-11 of sum p |v| where the output's own rounding is 2^-8 of its value, for half the
+// products with V.  Products, softmax and sums are fp32; log-sum-exps and weights take P before it is rounded.  V's exponents differ from block
 // to block: P goes in relative to 2^M, M a running maximum of logit + exponent, which keeps the largest terms of a row at
 // full precision whatever block they are in, and 2^5 times larger, so that 2^17 weights of 2^-26 are not lost beside one of
 // 1/2, as they are in an fp16 of at most 1.  References only move when they are exceeded by 2^10 (2^60 for the sums): until
@@ -29,8 +31,8 @@
 //
 // B200: 8 sequences of 32768 tokens, 8 heads of 128, one row of 32 query heads 89 us (537 MB of codes, 6.0 TB/s); one such
 // sequence with weights 22.6 us, of which about 7 are the launches' own; four rows of 28 query heads over 131072 tokens of 4 heads
-// 54 us (2.5 TB/s): there the instructions bound it, 1200 per warp and 32 tokens with two warps per scheduler (the accumulators
-// fill the registers).
+// 55 us (2.4 TB/s): latency.  The accumulators fill the registers, and the two warps per scheduler that this leaves issue in a third
+// of the cycles (mma pipe 31 %, DRAM 31 %): a step's products with K, its softmax and its products with V follow one another.
 #include <math.h>
 
 #include "cache8.cuh"
