@@ -367,7 +367,8 @@ KVC_API kvc_status kvc_rotary(const kvc_rope* rope, const kvc_rope_desc* desc, c
  * that is the larger one.  Rows behind a head's length are never read, and left as they are.
  * A cache holds finite numbers: an infinity becomes qmax with its sign, a NaN zero, and the exponent goes by
  * the values beside them; *device_status of the call that takes them in becomes KVC_ERR_NOT_FINITE unless it
- * holds an error already.  Codes that a caller writes must not be e4m3's NaN (0x7f, 0xff) or int8's -128.
+ * holds an error already.  (In e4m3 values from 1.9375 * 2^127 on round to 2^128, which is held but reads back
+ * as infinity.)  Codes that a caller writes must not be e4m3's NaN (0x7f, 0xff) or int8's -128.
  */
 typedef enum { KVC_INT8 = 0, KVC_E4M3 = 1 } kvc_cache_format;
 

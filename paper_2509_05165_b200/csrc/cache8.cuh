@@ -53,14 +53,14 @@ __device__ __forceinline__ float pow2_clamped(int e) { return pow2(min(max(e, -1
 
 // The smallest e with amax <= qmax 2^e: with amax = m 2^E, m in [1, 2), that is E minus the exponent of qmax, and one
 // more where m exceeds qmax's own significand (448 = 1.75 * 2^8, 127 = 1.984375 * 2^6).  Zero and subnormal amax end at
-// the lower bound, infinity at the upper one (codes under an exponent of 121 can stand for more than fp32 holds).
+// the lower bound.  `up`: amax (finite) stands for amax * 2^up; codes can stand for more than fp32 holds.
 template <int kFormat>
-__device__ __forceinline__ int exponent_of(float amax) {
+__device__ __forceinline__ int exponent_of(float amax, int up = 0) {
   const uint32_t b = __float_as_uint(amax);
-  const int E = (int)(b >> 23) - 127;
+  const int E = (int)(b >> 23) - 127 + up;
   const uint32_t m = b & 0x7fffffu;
   const int e = kFormat == KVC_E4M3 ? E - 8 + (m > 0x600000u) : E - 6 + (m > 0x7e0000u);
-  return E > 127 ? kExpMax : min(max(e, kExpMin), kExpMax);
+  return min(max(e, kExpMin), kExpMax);
 }
 
 // Codes of four values x * f (f a power of two, so the product is exact but for what rounds to zero): rounded to

@@ -307,17 +307,18 @@ evict_move_kernel(const __grid_constant__ EvictParams P, const int32_t* __restri
       vs_e[g] = P.src.v_exp[eb + (at[g] >> P.src.block_shift)];
     }
   }
+  constexpr int kDown = 8;                             // (448 * 2^121 and 2^-9 * 2^-100, both 2^-8 times, are normal fp32 numbers)
   float2 top = make_float2(0.f, 0.f);
 #pragma unroll
   for (int g = 0; g < 2; ++g) {
     const uint32_t km = max_codes<kFormat>(max_codes<kFormat>(max_codes<kFormat>(max_codes<kFormat>(0, kx[g].x), kx[g].y), kx[g].z), kx[g].w);
     const uint32_t vm = max_codes<kFormat>(max_codes<kFormat>(max_codes<kFormat>(max_codes<kFormat>(0, vx[g].x), vx[g].y), vx[g].z), vx[g].w);
-    top.x = fmaxf(top.x, max_value<kFormat>(km) * pow2_clamped(ks_e[g]));
-    top.y = fmaxf(top.y, max_value<kFormat>(vm) * pow2_clamped(vs_e[g]));
+    top.x = fmaxf(top.x, max_value<kFormat>(km) * pow2_clamped(ks_e[g] - kDown));
+    top.y = fmaxf(top.y, max_value<kFormat>(vm) * pow2_clamped(vs_e[g] - kDown));
   }
   top = job_max(top, j, scratch);
   if (row0 >= n) return;
-  const int ke = exponent_of<kFormat>(top.x), ve = exponent_of<kFormat>(top.y);
+  const int ke = exponent_of<kFormat>(top.x, kDown), ve = exponent_of<kFormat>(top.y, kDown);
   uint8_t *ko = P.dst.k + P.dst.base(unit), *vo = P.dst.v + P.dst.base(unit);
 #pragma unroll
   for (int g = 0; g < 2; ++g) {

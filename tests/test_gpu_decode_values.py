@@ -33,6 +33,27 @@ def test_evict_blocks_of_the_largest_exponent(dev, fmt):
     assert (dst.k_exp[..., :3] == 121).all() and (dst.v_exp[..., :3] == 121).all()
 
 
+@pytest.mark.parametrize("fmt", [I8, E4])
+def test_evict_values_next_to_the_types_largest(dev, fmt):
+    """bf16's largest value rounds to 2^128 in e4m3, which fp32 does not hold: its block still takes the smallest exponent that does."""
+    g = _gen(8)
+    x = [R.spread_rows(g, 1, 2, 64, 64).to(BF) for _ in range(2)]
+    x[0][..., 5, 3], x[1][..., 40, 60] = torch.finfo(BF).max, -torch.finfo(BF).max
+    c = kvc.alloc_cache(1, 2, 64, 64, 32, fmt, dev)
+    kvc.kvc_cache_append(c, x[0].to(dev), x[1].to(dev))
+    w = torch.rand((1, 2, 64), generator=g)
+    w[..., 5], w[..., 40] = 2.0, 2.0
+    dst, idx = kvc.alloc_cache(1, 2, 64, 40, 16, fmt, dev), torch.empty((1, 2, 40), dtype=torch.int32, device=dev)
+    kvc.kvc_evict(c, dst, w.to(dev), 40, 5, idx)
+    held = R.cache_values(c)
+    for j in range(2):
+        kept = idx[0, j].cpu().long()
+        for codes, exps, v in ((dst.k, dst.k_exp, held[0]), (dst.v, dst.v_exp, held[1])):
+            want = R.Held(fmt, 16).fill(v[0, j][kept])
+            assert exps[0, j].tolist() == want.exps
+            assert torch.equal(codes[0, j].cpu().double(), torch.cat(want.codes))
+
+
 # ---- rows that are not finite ------------------------------------------------------------------------------------------
 
 def _held(x, fmt):
